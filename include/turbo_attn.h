@@ -14,7 +14,10 @@
  *   - integer QK^T and PV contractions inside a FlashAttention-style tiled
  *     loop (Appendix A, Algorithm 1 prefill, Algorithm 2 decode).
  *
- * This header declares the three calls of that path plus their helpers.
+ * This header declares the three calls of that path plus their helpers, and
+ * serving calls over the same cache that the paper does not have: decoding from
+ * a choice of the cached groups (turbo_select_groups, turbo_attn_selected) and
+ * speculative decoding (turbo_tree_mask, turbo_attn_tree, turbo_append_path).
  *
  * General rules for every entry point
  *   - All tensor arguments are DEVICE pointers allocated and owned by the
@@ -51,6 +54,7 @@ extern "C" {
 #define TURBO_PAGES_PER_GROUP 4  /* TURBO_BLOCK / TURBO_PAGE_TOKENS */
 #define TURBO_MAX_KV_HEADS 64
 #define TURBO_MAX_GQA 16         /* max query heads per KV head */
+#define TURBO_MAX_TREE 256       /* max drafted nodes per sequence */
 
 /* Layout of the tile trace written by the *_trace test hooks (bytes), for a
  * tile of B_r query rows and B_c keys (B_r, B_c <= 128; 64 x 64 for the
@@ -501,6 +505,166 @@ int turbo_append_kv(const void* k_new, const void* v_new, int B, int Hkv, int d,
                     const int32_t* seq_lens, const turbo_kv_cache* cache,
                     const turbo_kv_tail* tail, const int32_t* block_table,
                     const int32_t* group_table, int max_groups_per_seq, hipStream_t stream);
+
+/*
+ * turbo_select_groups — the groups of the cache that a decoding step attends
+ * (not in the paper: sparse decoding).  A cheap score ranks the cached groups
+ * of every (sequence, KV head), from the step-2 metadata alone: the keys of a
+ * group lie, per channel, between z^int and z^int + L * s^int (L = 2^bits - 1).
+ * With the int8 codes q and scale s_Q of a query row (as turbo_attn_decode
+ * quantizes it),
+ *   I     = sum_c max(q_c * z_c, q_c * (z_c + L * s_c))     (an integer)
+ *   bound = fl(fl(fl(I) * s_Q) * s_K)                       (binary32)
+ *   score = max over the KV head's query rows of fl(bound - the row's largest
+ *           bound over the sequence's groups)
+ * so that every query row's best group scores 0.  A bound, difference or
+ * score that is not a number counts as -inf.  The num_select groups of
+ * largest score are chosen, equal scores by the lower index; the first
+ * keep_first and the last keep_last groups before all others.  Groups whose
+ * page or slot entries are out of range are never chosen.
+ *
+ * q               fp16 [B][Hq][128].
+ * cache, seq_lens, block_table, group_table, max_groups_per_seq
+ *                 as for turbo_attn_decode; the groups are the
+ *                 min(floor(seq_len/64), max_groups_per_seq) full ones.
+ * num_select      >= 1; keep_first, keep_last >= 0, together at most
+ *                 num_select.
+ * workspace       device scratch of turbo_select_workspace_bytes() bytes (no
+ *                 initialization needed); calls that share it must not overlap.
+ * selected        device int32 [B][Hkv][num_select] (output): the chosen
+ *                 groups in ascending order, then -1.
+ * B == 0 is a no-op.  WORKSPACE_TOO_SMALL for a missing or short workspace.
+ */
+int turbo_select_groups(const void* q, const turbo_kv_cache* cache, const int32_t* seq_lens,
+                        const int32_t* block_table, const int32_t* group_table,
+                        int max_groups_per_seq, int B, int Hq, int num_select, int keep_first,
+                        int keep_last, void* workspace, size_t workspace_bytes, int32_t* selected,
+                        hipStream_t stream);
+
+/* Workspace bytes of turbo_select_groups: fp32 [B][Hq][max_groups_per_seq] (0
+ * for arguments < 1). */
+size_t turbo_select_workspace_bytes(int B, int Hq, int max_groups_per_seq);
+
+/*
+ * turbo_attn_selected — one decoding step over chosen groups (not in the
+ * paper): each query row attends the tokens of its KV head's `selected` groups
+ * and, with a tail, the buffered tokens:
+ *   x_t = sm_scale * q . K_t,   o = sum_t e^(x_t) V_t / sum_t e^(x_t),
+ *   lse = ln sum_t e^(x_t),
+ * with K_t, V_t the values the cache stands for, (code * s^int + z^int) * s
+ * (code * s in the buffer), and the exponential itself: no n_r threshold, no
+ * quantization of q or of the probabilities.  Choosing every group is the
+ * attention that turbo_attn_decode approximates.  Sums are binary32; the
+ * probabilities are rounded to fp16 for the product with V.
+ *
+ * q, cache, tail, seq_lens, block_table, group_table, max_groups_per_seq
+ *                 as for turbo_attn_decode.
+ * selected        device int32 [B][Hkv][num_select]: groups of the sequence,
+ *                 in any order.  An entry outside 0 .. ng - 1 (ng the
+ *                 sequence's full groups) is skipped, as is a group whose table
+ *                 entries are out of range; a group named twice counts twice.
+ * num_select      >= 1.
+ * workspace       device scratch of turbo_selected_workspace_bytes() bytes
+ *                 (may be NULL when that is 0; no initialization needed); calls
+ *                 that share it must not overlap.
+ * o               fp16 [B][Hq][128];  lse fp32 [B][Hq] or NULL.  A row that
+ *                 attends no token yields o = 0 and lse = -inf.
+ * The same call on the same inputs gives the same bits; the order of the sums
+ * (not the result beyond rounding) depends on the shapes of the call.
+ */
+int turbo_attn_selected(const void* q, const turbo_kv_cache* cache, const turbo_kv_tail* tail,
+                        const int32_t* seq_lens, const int32_t* block_table,
+                        const int32_t* group_table, int max_groups_per_seq,
+                        const int32_t* selected, int num_select, int B, int Hq, float sm_scale,
+                        void* workspace, size_t workspace_bytes, void* o, float* lse,
+                        hipStream_t stream);
+
+/* Workspace bytes of turbo_attn_selected (with_tail = tail != NULL). */
+size_t turbo_selected_workspace_bytes(int B, int Hq, int Hkv, int num_select, int with_tail);
+
+/*
+ * turbo_tree_mask — ancestor bits of drafted trees (not in the paper:
+ * speculative decoding).
+ *
+ * parents    device int32 [B][T]: the parent of each node, an EARLIER node of
+ *            the same tree.  Any other value (-1, say) makes the node a root,
+ *            whose parent is the sequence's last token.
+ * tree_lens  device int32 [B]: nodes of each tree, 0 .. T (clamped).
+ * mask       device uint64 [B][T][ceil(T/64)] (output): bit j % 64 of word
+ *            j / 64 of node i is set where j is i or an ancestor of i.  Zero
+ *            for nodes past the tree's last.
+ * depth      device int32 [B][T] or NULL (output): the number of a node's
+ *            ancestors (its position is the sequence's length plus that); -1
+ *            past the last.
+ * T          1 .. TURBO_MAX_TREE.  B == 0 is a no-op.
+ */
+int turbo_tree_mask(const int32_t* parents, const int32_t* tree_lens, int B, int T, uint64_t* mask,
+                    int32_t* depth, hipStream_t stream);
+
+/*
+ * turbo_attn_tree — attention of drafted nodes (not in the paper): the T nodes
+ * of each sequence, none of them in the cache yet, attend all its tokens in the
+ * cache and the buffer, and the nodes their mask names, in one call:
+ *   x_t = sm_scale * q . K_t,   o = sum_t e^(x_t) V_t / sum_t e^(x_t)
+ * over those tokens, with the values and the arithmetic of
+ * turbo_attn_selected; the nodes' keys and values are taken as they are (fp16).
+ *
+ * q          fp16 [B][Hq][T][128].
+ * k_tree,
+ * v_tree     fp16 [B][Hkv][T][128]: the nodes' keys and values.
+ * tree_mask  device uint64 [B][T][ceil(T/64)], as written by turbo_tree_mask
+ *            or by the caller: node i attends the nodes whose bits are set,
+ *            itself among them only if its own is.  Bits of nodes past the
+ *            tree's last are ignored.  NULL: node i attends nodes 0 .. i (a
+ *            chain).
+ * tree_lens  device int32 [B]: nodes of each tree, 0 .. T (clamped).
+ * cache, tail, seq_lens, block_table, group_table, max_groups_per_seq
+ *            as for turbo_attn_decode.
+ * T          1 .. TURBO_MAX_TREE.
+ * workspace  device scratch of turbo_tree_workspace_bytes() bytes (may be NULL
+ *            when that is 0; no initialization needed); calls that share it
+ *            must not overlap.
+ * o          fp16 [B][Hq][T][128];  lse fp32 [B][Hq][T] or NULL.  A row that
+ *            attends no token yields o = 0 and lse = -inf.  Rows of nodes past
+ *            a tree's last are left as they were.
+ * A key or value of a node that a row does not attend, and anything past the
+ * tree's last node, has no effect on it, be it infinite or NaN.
+ */
+int turbo_attn_tree(const void* q, const void* k_tree, const void* v_tree,
+                    const uint64_t* tree_mask, const int32_t* tree_lens,
+                    const turbo_kv_cache* cache, const turbo_kv_tail* tail,
+                    const int32_t* seq_lens, const int32_t* block_table,
+                    const int32_t* group_table, int max_groups_per_seq, int B, int Hq, int T,
+                    float sm_scale, void* workspace, size_t workspace_bytes, void* o, float* lse,
+                    hipStream_t stream);
+
+/* Workspace bytes of turbo_attn_tree (with_tail = tail != NULL). */
+size_t turbo_tree_workspace_bytes(int B, int Hq, int Hkv, int T, int max_groups_per_seq,
+                                  int with_tail);
+
+/*
+ * turbo_append_path — append of accepted nodes (not in the paper): the nodes
+ * path[b][0 .. path_lens[b] - 1] of sequence b become its tokens at positions
+ * seq_lens[b] onwards.  The buffer and the cache are then, bit for bit, what one
+ * turbo_append_kv per node (with the lengths advanced in between) leaves: every
+ * buffer that fills up on the way is compressed into its group.  The caller
+ * advances seq_lens afterwards.
+ *
+ * k_tree,
+ * v_tree     fp16 [B][Hkv][T][128], as given to turbo_attn_tree.
+ * path       device int32 [B][max_path].  The path ends before an entry outside
+ *            0 .. T - 1; a node may come up more than once.
+ * path_lens  device int32 [B], clamped to 0 .. max_path.
+ * seq_lens   device int32 [B]: lengths before the call (< 0 skips the sequence).
+ * cache, tail, block_table, group_table, max_groups_per_seq
+ *            as for turbo_append_kv.
+ * B == 0 is a no-op.
+ */
+int turbo_append_path(const void* k_tree, const void* v_tree, int B, int Hkv, int T, int d,
+                      const int32_t* path, const int32_t* path_lens, int max_path,
+                      const int32_t* seq_lens, const turbo_kv_cache* cache,
+                      const turbo_kv_tail* tail, const int32_t* block_table,
+                      const int32_t* group_table, int max_groups_per_seq, hipStream_t stream);
 
 /*
  * turbo_sas_softmax — Algorithm 3 (Appendix B; SAS of Sec. 4) as a

@@ -20,6 +20,7 @@ HEAD_DIM = 128
 BLOCK = 64
 PAGE_TOKENS = 16
 MAX_KV_HEADS = 64
+MAX_TREE = 256
 # tile trace layout of the *_trace test hooks (include/turbo_attn.h)
 TRACE_Q8, TRACE_S, TRACE_P, TRACE_PV, TRACE_SQ, TRACE_PMAX, TRACE_BYTES = (
     0, 16384, 81920, 98304, 163840, 163844, 163848)
@@ -85,6 +86,14 @@ def lib() -> ctypes.CDLL:
             "turbo_probe_read": ([P, Z, P, P], I),
             "turbo_probe_valu": ([I, P, P, P], I),
             "turbo_decode_workspace_bytes": ([I, I, I, I, I, I], Z),
+            "turbo_select_groups": ([P, P, P, P, P, I, I, I, I, I, I, P, Z, P, P], I),
+            "turbo_select_workspace_bytes": ([I, I, I], Z),
+            "turbo_attn_selected": ([P, P, P, P, P, P, I, P, I, I, I, F, P, Z, P, P, P], I),
+            "turbo_selected_workspace_bytes": ([I, I, I, I, I], Z),
+            "turbo_tree_mask": ([P, P, I, I, P, P, P], I),
+            "turbo_attn_tree": ([P, P, P, P, P, P, P, P, P, P, I, I, I, I, F, P, Z, P, P, P], I),
+            "turbo_tree_workspace_bytes": ([I, I, I, I, I, I], Z),
+            "turbo_append_path": ([P, P, I, I, I, I, P, P, I, P, P, P, P, P, I, P], I),
         }
         for name, (args, res) in sig.items():
             fn = getattr(L, name)
@@ -511,6 +520,208 @@ def turbo_attn_prefill_q8(q8: torch.Tensor, s_q: torch.Tensor, k8, v8, s_k, s_v,
                                        _ptr(o), _ptr(lse), _stream(q8.device)),
            "turbo_attn_prefill_q8")
     return (o, lse) if return_lse else o
+
+
+# ---- sparse and speculative decoding -------------------------------------------
+# These calls check every tensor (type, shape, device, contiguity) and run on the
+# tensors' device, whichever is current.
+
+
+def _arg(t: torch.Tensor, name: str, dtype, shape, device) -> int:
+    """Address of t, which must have this type and shape and lie on device."""
+    if t.dtype != dtype or t.shape != shape or t.device != device:
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on {device}, but is {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _shape(t: torch.Tensor, name: str, dims: int):
+    if t.dim() != dims:
+        raise ValueError(f"{name} must have {dims} dimensions, but is {tuple(t.shape)}")
+    return t.shape
+
+
+def _cache_args(cache: PagedKVCache, tail: Optional[KVTail], B: int, seq_lens: torch.Tensor,
+                block_table: torch.Tensor, group_table: torch.Tensor, device):
+    """(cache struct, tail struct, lengths, block table, group table, max_groups)."""
+    mg = _shape(group_table, "group_table", 2)[1]
+    for t in (cache.pages, cache.group_meta, cache.group_scale):
+        if t.device != device or not t.is_contiguous():
+            raise ValueError(f"the cache must be contiguous on {device}")
+    ts = None
+    if tail is not None:
+        for t in (tail.k, tail.v, tail.scale):
+            if t.device != device or not t.is_contiguous():
+                raise ValueError(f"the buffer must be contiguous on {device}")
+        ts = tail._packed()
+    i32 = torch.int32
+    return (cache._packed(), ts, _arg(seq_lens, "seq_lens", i32, (B,), device),
+            _arg(block_table, "block_table", i32, (B, 4 * mg), device),
+            _arg(group_table, "group_table", i32, (B, mg), device), mg)
+
+
+def _scratch(workspace: Optional[torch.Tensor], device):
+    """(address, bytes) of a workspace."""
+    if workspace is None:
+        return None, 0
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on {device}")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _launch(device, what: str, *args):
+    """The library's `what` with args and the device's current stream, on that device."""
+    stream = _stream(device)
+    fn = getattr(lib(), what)
+    if device.index == torch.cuda.current_device():
+        status = fn(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, stream)
+    _check(status, what)
+
+
+def _words(nbytes: int, device) -> Optional[torch.Tensor]:
+    return torch.empty(nbytes // 4, dtype=torch.float32, device=device) if nbytes else None
+
+
+def select_workspace(B: int, Hq: int, max_groups: int, device="cuda") -> Optional[torch.Tensor]:
+    return _words(int(lib().turbo_select_workspace_bytes(B, Hq, max_groups)), device)
+
+
+def selected_workspace(B: int, Hq: int, Hkv: int, num_select: int, device="cuda",
+                       with_tail: bool = False) -> Optional[torch.Tensor]:
+    return _words(int(lib().turbo_selected_workspace_bytes(B, Hq, Hkv, num_select,
+                                                           int(bool(with_tail)))), device)
+
+
+def tree_workspace(B: int, Hq: int, Hkv: int, T: int, max_groups: int, device="cuda",
+                   with_tail: bool = False) -> Optional[torch.Tensor]:
+    return _words(int(lib().turbo_tree_workspace_bytes(B, Hq, Hkv, T, max_groups,
+                                                       int(bool(with_tail)))), device)
+
+
+def turbo_select_groups(q: torch.Tensor, cache: PagedKVCache, seq_lens: torch.Tensor,
+                        block_table: torch.Tensor, group_table: torch.Tensor, num_select: int,
+                        keep_first: int = 1, keep_last: int = 1,
+                        workspace: Optional[torch.Tensor] = None, out=None) -> torch.Tensor:
+    """The num_select cached groups of each (sequence, KV head) whose metadata
+    bounds the scores of q fp16 [B][Hq][128] highest (the first keep_first and
+    last keep_last always).  Returns int32 [B][Hkv][num_select], ascending, -1
+    behind the last."""
+    B, Hq, d = _shape(q, "q", 3)
+    dev, Hkv = q.device, cache.num_kv_heads
+    qp = _arg(q, "q", torch.float16, (B, Hq, HEAD_DIM), dev)
+    cs, _, sl, bt, gt, mg = _cache_args(cache, None, B, seq_lens, block_table, group_table, dev)
+    if num_select < 1:
+        raise ValueError("num_select must be at least 1")
+    sel = torch.empty(B, Hkv, num_select, dtype=torch.int32, device=dev) if out is None else out
+    sp = _arg(sel, "out", torch.int32, (B, Hkv, num_select), dev)
+    if workspace is None:
+        workspace = select_workspace(B, Hq, mg, dev)
+    wp, wbytes = _scratch(workspace, dev)
+    _launch(dev, "turbo_select_groups", qp, cs, sl, bt, gt, mg, B, Hq, int(num_select),
+            int(keep_first), int(keep_last), wp, wbytes, sp)
+    return sel
+
+
+def turbo_attn_selected(q: torch.Tensor, cache: PagedKVCache, seq_lens: torch.Tensor,
+                        block_table: torch.Tensor, group_table: torch.Tensor,
+                        selected: torch.Tensor, sm_scale: Optional[float] = None,
+                        workspace: Optional[torch.Tensor] = None, return_lse: bool = False,
+                        out=None, lse_out=None, tail: Optional[KVTail] = None):
+    """Attention of q fp16 [B][Hq][128] over the groups `selected` int32
+    [B][Hkv][num_select] of the cache (and the buffer when tail is given), with
+    the exponential itself.  Returns o (and lse)."""
+    B, Hq, d = _shape(q, "q", 3)
+    dev, Hkv = q.device, cache.num_kv_heads
+    qp = _arg(q, "q", torch.float16, (B, Hq, HEAD_DIM), dev)
+    cs, ts, sl, bt, gt, mg = _cache_args(cache, tail, B, seq_lens, block_table, group_table, dev)
+    k = _shape(selected, "selected", 3)[2]
+    sp = _arg(selected, "selected", torch.int32, (B, Hkv, k), dev)
+    o = torch.empty_like(q) if out is None else out
+    op = _arg(o, "out", torch.float16, q.shape, dev)
+    lse = lse_out
+    if lse is None and return_lse:
+        lse = torch.empty(B, Hq, dtype=torch.float32, device=dev)
+    lp = None if lse is None else _arg(lse, "lse_out", torch.float32, (B, Hq), dev)
+    if workspace is None:
+        workspace = selected_workspace(B, Hq, Hkv, k, dev, tail is not None)
+    wp, wbytes = _scratch(workspace, dev)
+    _launch(dev, "turbo_attn_selected", qp, cs, ts, sl, bt, gt, mg, sp, k, B, Hq,
+            _scale(HEAD_DIM, sm_scale), wp, wbytes, op, lp)
+    return o if lse is None else (o, lse)
+
+
+def turbo_tree_mask(parents: torch.Tensor, tree_lens: torch.Tensor, out=None, depth_out=None):
+    """Ancestor bits int64 [B][T][ceil(T/64)] and depths int32 [B][T] of drafted
+    trees, from parents int32 [B][T] (an earlier node, or -1) and tree_lens int32
+    [B]."""
+    B, T = _shape(parents, "parents", 2)
+    dev = parents.device
+    pp = _arg(parents, "parents", torch.int32, (B, T), dev)
+    lp = _arg(tree_lens, "tree_lens", torch.int32, (B,), dev)
+    W = (T + 63) // 64
+    mask = torch.empty(B, T, W, dtype=torch.int64, device=dev) if out is None else out
+    depth = torch.empty(B, T, dtype=torch.int32, device=dev) if depth_out is None else depth_out
+    _launch(dev, "turbo_tree_mask", pp, lp, B, T, _arg(mask, "out", torch.int64, (B, T, W), dev),
+            _arg(depth, "depth_out", torch.int32, (B, T), dev))
+    return mask, depth
+
+
+def turbo_attn_tree(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor,
+                    tree_mask: Optional[torch.Tensor], tree_lens: torch.Tensor,
+                    cache: PagedKVCache, seq_lens: torch.Tensor, block_table: torch.Tensor,
+                    group_table: torch.Tensor, sm_scale: Optional[float] = None,
+                    workspace: Optional[torch.Tensor] = None, return_lse: bool = False, out=None,
+                    lse_out=None, tail: Optional[KVTail] = None):
+    """Attention of drafted nodes, q fp16 [B][Hq][T][128], over the cache (and the
+    buffer when tail is given) and over the nodes k_tree, v_tree fp16
+    [B][Hkv][T][128] that tree_mask int64 [B][T][ceil(T/64)] names (None: the nodes
+    up to the row's own), with the exponential itself.  Rows of nodes from
+    tree_lens[b] on are not written.  Returns o (and lse)."""
+    B, Hq, T, d = _shape(q, "q", 4)
+    dev, Hkv, f16 = q.device, cache.num_kv_heads, torch.float16
+    qp = _arg(q, "q", f16, (B, Hq, T, HEAD_DIM), dev)
+    kp = _arg(k_tree, "k_tree", f16, (B, Hkv, T, HEAD_DIM), dev)
+    vp = _arg(v_tree, "v_tree", f16, (B, Hkv, T, HEAD_DIM), dev)
+    mp = None
+    if tree_mask is not None:
+        mp = _arg(tree_mask, "tree_mask", torch.int64, (B, T, (T + 63) // 64), dev)
+    tp = _arg(tree_lens, "tree_lens", torch.int32, (B,), dev)
+    cs, ts, sl, bt, gt, mg = _cache_args(cache, tail, B, seq_lens, block_table, group_table, dev)
+    o = torch.empty_like(q) if out is None else out
+    op = _arg(o, "out", f16, q.shape, dev)
+    lse = lse_out
+    if lse is None and return_lse:
+        lse = torch.empty(B, Hq, T, dtype=torch.float32, device=dev)
+    lp = None if lse is None else _arg(lse, "lse_out", torch.float32, (B, Hq, T), dev)
+    if workspace is None:
+        workspace = tree_workspace(B, Hq, Hkv, T, mg, dev, tail is not None)
+    wp, wbytes = _scratch(workspace, dev)
+    _launch(dev, "turbo_attn_tree", qp, kp, vp, mp, tp, cs, ts, sl, bt, gt, mg, B, Hq, T,
+            _scale(HEAD_DIM, sm_scale), wp, wbytes, op, lp)
+    return o if lse is None else (o, lse)
+
+
+def turbo_append_path(k_tree: torch.Tensor, v_tree: torch.Tensor, path: torch.Tensor,
+                      path_lens: torch.Tensor, seq_lens: torch.Tensor, cache: PagedKVCache,
+                      tail: KVTail, block_table: torch.Tensor, group_table: torch.Tensor):
+    """Append of accepted nodes: path int32 [B][max_path] (path_lens int32 [B] of
+    them) of k_tree, v_tree fp16 [B][Hkv][T][128] at positions seq_lens onwards, as
+    one turbo_append_kv each would."""
+    B, Hkv, T, d = _shape(k_tree, "k_tree", 4)
+    dev = k_tree.device
+    kp = _arg(k_tree, "k_tree", torch.float16, (B, Hkv, T, HEAD_DIM), dev)
+    vp = _arg(v_tree, "v_tree", torch.float16, (B, Hkv, T, HEAD_DIM), dev)
+    P = _shape(path, "path", 2)[1]
+    pp = _arg(path, "path", torch.int32, (B, P), dev)
+    lp = _arg(path_lens, "path_lens", torch.int32, (B,), dev)
+    cs, ts, sl, bt, gt, mg = _cache_args(cache, tail, B, seq_lens, block_table, group_table, dev)
+    _launch(dev, "turbo_append_path", kp, vp, B, Hkv, T, HEAD_DIM, pp, lp, P, sl, cs, ts, bt, gt,
+            mg)
 
 
 def probe_mfma_i8(iters: int, device="cuda") -> int:

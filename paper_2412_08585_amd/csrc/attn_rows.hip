@@ -1,0 +1,705 @@
+// Attention of several query rows per sequence over the paged int4/int2 cache,
+// with the exponential itself: the drafted nodes of a tree (turbo_attn_tree), or
+// one row per query head over a choice of groups (turbo_attn_selected).
+//
+// For a row with query q and a visible token t,
+//   x_t = sm_scale * q . K_t,   o = sum_t e^(x_t) V_t / sum_t e^(x_t),
+// K_t, V_t the values the cache stands for: (code * s^int + z^int) * s for a
+// cached group, code * s for the buffer, fp16 for a drafted node.  One pass over
+// the tokens in tiles of 64 with the running maximum m and sum l of each row,
+// everything in binary32 but the operands of the matrix instructions:
+//  * K and V as fp16 integers code * s^int + z^int (|.| <= 2048: exact), q as
+//    given: the products of Q K^T are exact, their sums binary32;
+//  * P = 2^(x - m + 15), rounded to fp16 (relative 2^-11, as the output's own
+//    rounding); the 2^15 keeps terms down to 2^-29 of the row's largest in fp16's
+//    normal range.  l sums P before it is rounded.
+//
+// The tokens of the G query heads of a KV head are one matrix of G * T rows.  A
+// wave takes 16 of them and a tile:
+//   S^T = K q^T   (16x16x32 fp16 MFMA; A row m of block mb: token
+//                  16 (m >> 2) + 4 mb + (m & 3) of the tile)
+//   O^T += V^T P^T (A row m of block cb: channel 8 m + cb)
+// With this order of tokens lane (n, g4) -- n = lane & 15 the query row, g4 =
+// lane >> 4 -- holds the scores of the 16 tokens of page g4, which are the ones
+// its operand of the second product needs: P never leaves the registers, and the
+// row's m and l are the lane's own.  With this order of channels a lane's codes of
+// V are one run of its page, and its outputs runs of 8 channels.
+#include "turbo_common.h"
+#include "stream_loads.h"
+
+namespace turbo {
+
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+// q, the nodes' keys and values and o may lie at any fp16 boundary
+typedef unsigned u4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+struct RowsArgs {
+  const unsigned short* q;   // fp16 [B][Hq][T][128]
+  const unsigned short* kt;  // fp16 [B][Hkv][T][128] (null: no nodes)
+  const unsigned short* vt;
+  const unsigned long long* mask;  // [B][T][mwords]; null: node i sees 0 .. i
+  int mwords;
+  const int* tree_lens;      // [B]; null: T
+  const int* sel;            // [B][Hkv][nsel] groups to attend; null: all
+  int nsel;
+  const uint8_t* pages;
+  const int8_t* gmeta;       // [slots][Hkv][4][128]
+  const float* gscale;       // [slots][Hkv][2]
+  int npages, nslots;        // min(num_pages, INT_MAX), min(num_slots, INT_MAX)
+  int page_bytes;
+  unsigned long long int2_mask;
+  const int* seq_lens;       // [B]
+  const int* block_table;    // [B][4*max_groups]
+  const int* group_table;    // [B][max_groups]
+  int max_groups;
+  int B, Hq, Hkv, G, T;
+  float sm_log2e;            // sm_scale * log2(e)
+  const int8_t* tk;          // Sec. 3.3 buffer (null: none)
+  const int8_t* tv;
+  const float* tscale;
+  int ntiles_row;            // row tiles in the grid
+  int nchunk;                // chunks in the grid
+  float* ws;                 // [B][Hq][T][nchunk][132]: m, l, -, -, O[128]
+  unsigned short* o;         // fp16 [B][Hq][T][128]
+  float* lse;                // [B][Hq][T] or null
+};
+
+constexpr int kRowsWaves = 4;   // waves of a work-group, a tile each in turn
+constexpr float kPShift = 15.0f;
+
+// The tiles of sequence b: cached groups (or choices), the buffer, the nodes.
+struct RowsSeq {
+  int ng;      // cached groups
+  int nt;      // buffered tokens
+  int tl;      // nodes
+  int nlist;   // tiles of cached groups
+  int ntile;   // all tiles
+  int len;     // tiles of a chunk
+  int nparts;  // chunks
+};
+
+__device__ __forceinline__ RowsSeq rows_seq(const RowsArgs& a, int b) {
+  RowsSeq s;
+  const int len = a.seq_lens[b];
+  s.ng = min(max(len / 64, 0), a.max_groups);
+  s.nt = a.tk ? min(max(len - 64 * s.ng, 0), 63) : 0;
+  s.tl = a.tree_lens ? min(max(a.tree_lens[b], 0), a.T) : a.T;
+  s.nlist = a.sel ? a.nsel : s.ng;
+  s.ntile = s.nlist + (s.nt > 0) + (a.kt ? (s.tl + 63) / 64 : 0);
+  s.len = max(kRowsWaves, ceil_div(s.ntile, a.nchunk));
+  s.nparts = ceil_div(s.ntile, s.len);
+  return s;
+}
+
+__device__ __forceinline__ f4 mfma_h(u32x4_t a, u32x4_t b, f4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a),
+                                                __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ unsigned h2_fma(unsigned a, unsigned b, unsigned c) {
+  return __builtin_bit_cast(
+      unsigned, __builtin_elementwise_fma(__builtin_bit_cast(h2, a), __builtin_bit_cast(h2, b),
+                                          __builtin_bit_cast(h2, c)));
+}
+__device__ __forceinline__ unsigned h2_add(unsigned a, unsigned b) {
+  return __builtin_bit_cast(unsigned, __builtin_bit_cast(h2, a) + __builtin_bit_cast(h2, b));
+}
+__device__ __forceinline__ unsigned h2_of(float lo, float hi) {
+  const h2 x = {(_Float16)lo, (_Float16)hi};
+  return __builtin_bit_cast(unsigned, x);
+}
+
+// Codes to fp16.  Pair i of a word (int4: nibbles i, i + 4; int2: fields i, i + 8)
+// goes to the top mantissa bits of the two halves of 1.0: 1 + code / 2^bits.  With
+// s' = 2^bits s and z' = z - 2^bits s, fma(1 + code / 2^bits, s', z') = code s + z,
+// an integer: exact while s' + |z| <= 2048, as in every group this library writes
+// (s <= 16 with 4 bits, 80 with 2).
+template <int BITS>
+__device__ __forceinline__ unsigned code_pair(unsigned w, int i) {
+  constexpr int at = 10 - BITS;  // bit of the field in the half
+  const int sh = BITS * i - at;
+  const unsigned x = sh > 0 ? w >> sh : w << -sh;
+  constexpr unsigned m = BITS == 4 ? 0x03C003C0u : 0x03000300u;
+  return (x & m) | 0x3C003C00u;
+}
+
+// s' and z' of two channels, their s^int and z^int bytes in bits 0-7 and 16-23 of
+// s and z.  (0x6400 | x is 1024 + x.)
+template <int BITS>
+__device__ __forceinline__ void scale_pair(unsigned s, unsigned z, unsigned& sp, unsigned& zp) {
+  constexpr float f = 1 << BITS;
+  sp = h2_fma(s | 0x64006400u, h2_of(f, f), h2_of(-1024.0f * f, -1024.0f * f));
+  const unsigned zi = h2_add((z ^ 0x00800080u) | 0x64006400u, h2_of(-1152.0f, -1152.0f));
+  zp = h2_add(zi, sp ^ 0x80008000u);
+}
+
+// int8 pair (bytes at bits 0-7 and 16-23, high bits flipped) to fp16.
+__device__ __forceinline__ unsigned int8_pair(unsigned x) {
+  return h2_add(x | 0x64006400u, h2_of(-1152.0f, -1152.0f));
+}
+
+// Order of a tile's 32 channels of lane group g4 over the four k-steps: register jj
+// of step ks holds channels 32 g4 + first(ks, jj) and that + dist.
+enum { kOrd4 = 0, kOrd2 = 1, kOrdNat = 2 };
+template <int ORD>
+__device__ __forceinline__ int chan_lo(int ks, int jj) {
+  return ORD == kOrd4 ? 8 * ks + jj : ORD == kOrd2 ? 16 * (ks >> 1) + 4 * (ks & 1) + jj : 8 * ks + 2 * jj;
+}
+template <int ORD>
+constexpr int kChanDist = ORD == kOrd4 ? 4 : (ORD == kOrd2 ? 8 : 1);
+
+// The wave's query rows as the B operand of S^T, in one of these orders.
+template <int NT>
+struct RowsQ {
+  u32x4_t x[NT][4];
+  long at[NT];  // row of q, o and lse; -1 past the last
+  int node[NT];
+};
+
+template <int NT, int ORD>
+__device__ __forceinline__ void load_q(const RowsArgs& a, RowsQ<NT>& Q) {
+  const int g4 = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    unsigned raw[16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      u4_any x = {0, 0, 0, 0};
+      if (Q.at[t] >= 0) x = reinterpret_cast<const u4_any*>(a.q + Q.at[t] * 128 + 32 * g4)[i];
+      raw[4 * i] = x.x; raw[4 * i + 1] = x.y; raw[4 * i + 2] = x.z; raw[4 * i + 3] = x.w;
+    }
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj) {
+        const int c = chan_lo<ORD>(ks, jj);
+        if (ORD == kOrdNat) {
+          Q.x[t][ks][jj] = raw[c >> 1];
+        } else {
+          const unsigned lo = raw[c >> 1], hi = raw[(c + kChanDist<ORD>) >> 1];
+          Q.x[t][ks][jj] = __builtin_amdgcn_perm(hi, lo, c & 1 ? 0x07060302u : 0x05040100u);
+        }
+      }
+  }
+}
+
+// Running state of the wave's rows: O^T (channel 32 g4 + 8 r + cb in O[t][cb][r]),
+// maximum (in units of log2) and this lane's part of the sum.
+template <int NT>
+struct RowsState {
+  f4 o[NT][8];
+  float m[NT], l[NT];
+};
+
+// Scores to probabilities: S holds the products of row tile t, x = S * c2; bit
+// 4 mb + r of vis says whether token (mb, r) of the lane's page is visible.  Rescales
+// the state and returns P as the B operand of O^T: PAIR4 pairs tokens (8 ks + jj,
+// + 4) of the page, else (4 ks + jj, + 8).
+template <int NT, bool PAIR4>
+__device__ __forceinline__ void rows_softmax(RowsState<NT>& st, int t, f4 (&S)[4], float c2,
+                                             unsigned vis, u32x4_t (&P)[2]) {
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float x = S[mb][r] * c2;
+      S[mb][r] = (vis >> (4 * mb + r)) & 1u ? x : -INFINITY;
+    }
+  float mx = S[0][0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) mx = fmaxf(mx, S[i >> 2][i & 3]);
+  mx = max_xor32(max_xor16(mx));
+  const float mo = st.m[t], mn = fmaxf(mo, mx);
+  st.m[t] = mn;
+  if (__any(mn != mo)) {
+    // (a row that has seen nothing yet: its sums are zero)
+    const float al = mo == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mo - mn);
+    st.l[t] *= al;
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb) st.o[t][cb] *= al;
+  }
+  const float off = mn == -INFINITY ? 0.0f : kPShift - mn;
+  float l = 0.0f;
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      S[mb][r] = __builtin_amdgcn_exp2f(S[mb][r] + off);
+      l += S[mb][r];
+    }
+  st.l[t] += l;
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+    for (int jj = 0; jj < 4; ++jj)
+      P[ks][jj] = PAIR4 ? h2_of(S[2 * ks][jj], S[2 * ks + 1][jj]) : h2_of(S[ks][jj], S[ks + 2][jj]);
+}
+
+// ---- a cached group ------------------------------------------------------------
+template <int BITS>
+struct RowsGroup {
+  bool ok;
+  unsigned k[4][BITS];     // codes of token (m, mb), the lane's 32 channels
+  unsigned v[8 * BITS / 2];  // codes of channels 8 n .. 8 n + 7, the lane's page
+  uint2 ks, kz;            // s^int, z^int of the 8 channels that hold the lane's pair
+  uint2 vs, vz;            // of channels 8 n .. 8 n + 7
+  float sk, sv;
+};
+
+template <int BITS>
+__device__ __forceinline__ void load_group(const RowsArgs& a, int b, int kh, int head_off, int g,
+                                           RowsGroup<BITS>& x) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
+  const int* bt = a.block_table + (long)b * 4 * a.max_groups + 4L * g;
+  const int slot = a.group_table[(long)b * a.max_groups + g];
+  bool ok = slot >= 0 && slot < a.nslots;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) ok = ok && bt[i] >= 0 && bt[i] < a.npages;
+  x.ok = ok;
+  if (!ok) return;  // skipped: nothing of it is read
+  const uint8_t* kp = a.pages + (long)bt[n >> 2] * a.page_bytes + head_off + (n & 3) * 16 * BITS + 4 * BITS * g4;
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb) {
+    if constexpr (BITS == 4) {
+      const u32x4_t w = load_nt4(kp + 4 * mb * 16 * BITS);
+      x.k[mb][0] = w.x; x.k[mb][1] = w.y; x.k[mb][2] = w.z; x.k[mb][3] = w.w;
+    } else {
+      const u32x2_t w = load_nt2(kp + 4 * mb * 16 * BITS);
+      x.k[mb][0] = w.x; x.k[mb][1] = w.y;
+    }
+  }
+  const uint8_t* vp = a.pages + (long)bt[g4] * a.page_bytes + head_off + 256 * BITS + n * 16 * BITS;
+#pragma unroll
+  for (int i = 0; i < BITS; ++i) {
+    const u32x4_t w = load_nt4(vp + 16 * i);
+    x.v[4 * i] = w.x; x.v[4 * i + 1] = w.y; x.v[4 * i + 2] = w.z; x.v[4 * i + 3] = w.w;
+  }
+  const int8_t* meta = a.gmeta + ((long)slot * a.Hkv + kh) * 512;
+  // the lane converts pair (ks, jj) = (n >> 2, n & 3) of its channels
+  constexpr int ORD = BITS == 4 ? kOrd4 : kOrd2;
+  const int c = 32 * g4 + (chan_lo<ORD>(n >> 2, n & 3) & ~3);
+  x.ks = make_uint2(*reinterpret_cast<const unsigned*>(meta + c),
+                    *reinterpret_cast<const unsigned*>(meta + c + kChanDist<ORD>));
+  x.kz = make_uint2(*reinterpret_cast<const unsigned*>(meta + 128 + c),
+                    *reinterpret_cast<const unsigned*>(meta + 128 + c + kChanDist<ORD>));
+  x.vs = *reinterpret_cast<const uint2*>(meta + 256 + 8 * n);
+  x.vz = *reinterpret_cast<const uint2*>(meta + 384 + 8 * n);
+  const float* gs = a.gscale + ((long)slot * a.Hkv + kh) * 2;
+  x.sk = gs[0];
+  x.sv = gs[1];
+}
+
+template <int BITS, int NT>
+__device__ __forceinline__ void step_group(const RowsArgs& a, const RowsGroup<BITS>& x,
+                                           const RowsQ<NT>& Q, RowsState<NT>& st, uint2* szk) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
+  // s' and z' of the lane group's channel pairs, exchanged through LDS
+  {
+    const int sh = 8 * (n & 3);
+    unsigned sp, zp;
+    scale_pair<BITS>(((x.ks.x >> sh) & 0xffu) | (((x.ks.y >> sh) & 0xffu) << 16),
+                     ((x.kz.x >> sh) & 0xffu) | (((x.kz.y >> sh) & 0xffu) << 16), sp, zp);
+    wave_sync();
+    szk[lane] = make_uint2(sp, zp);
+    wave_sync();
+  }
+  f4 S[NT][4];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb) S[t][mb] = f4{0, 0, 0, 0};
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) {
+    uint2 sz[4];
+#pragma unroll
+    for (int jj = 0; jj < 4; ++jj) sz[jj] = szk[16 * g4 + 4 * ks + jj];
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb) {
+      u32x4_t A;
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj) {
+        const unsigned c = BITS == 4 ? code_pair<BITS>(x.k[mb][ks], jj)
+                                     : code_pair<BITS>(x.k[mb][ks >> 1], 4 * (ks & 1) + jj);
+        A[jj] = h2_fma(c, sz[jj].x, sz[jj].y);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) S[t][mb] = mfma_h(A, Q.x[t][ks], S[t][mb]);
+    }
+  }
+  u32x4_t P[NT][2];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+    rows_softmax<NT, BITS == 4>(st, t, S[t], x.sk * a.sm_log2e, 0xffffu, P[t]);
+#pragma unroll
+  for (int cb = 0; cb < 8; ++cb) {
+    const unsigned sel = 0x0c000c00u | (unsigned)(cb & 3) | (unsigned)(cb & 3) << 16;
+    unsigned sp, zp;
+    scale_pair<BITS>(__builtin_amdgcn_perm(0u, cb < 4 ? x.vs.x : x.vs.y, sel),
+                     __builtin_amdgcn_perm(0u, cb < 4 ? x.vz.x : x.vz.y, sel), sp, zp);
+    f4 acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f4{0, 0, 0, 0};
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      u32x4_t A;
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj) {
+        const unsigned c = BITS == 4 ? code_pair<BITS>(x.v[2 * cb + ks], jj)
+                                     : code_pair<BITS>(x.v[cb], 4 * ks + jj);
+        A[jj] = h2_fma(c, sp, zp);
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[t] = mfma_h(A, P[t][ks], acc[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st.o[t][cb][r] = __builtin_fmaf(acc[t][r], x.sv, st.o[t][cb][r]);
+  }
+}
+
+// ---- the int8 buffer ---------------------------------------------------------------
+// Q in order kOrd4.
+template <int NT>
+__device__ __forceinline__ void step_buffer(const RowsArgs& a, long u, int nt, const RowsQ<NT>& Q,
+                                            RowsState<NT>& st) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
+  f4 S[NT][4];
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb) {
+    const int8_t* kr = a.tk + (u * 64 + 16 * (n >> 2) + 4 * mb + (n & 3)) * 128 + 32 * g4;
+    unsigned w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = reinterpret_cast<const unsigned*>(kr)[i] ^ 0x80808080u;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) S[t][mb] = f4{0, 0, 0, 0};
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      u32x4_t A;
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj)
+        A[jj] = int8_pair(__builtin_amdgcn_perm(w[2 * ks + 1], w[2 * ks], 0x0c040c00u + 0x00010001u * jj));
+#pragma unroll
+      for (int t = 0; t < NT; ++t) S[t][mb] = mfma_h(A, Q.x[t][ks], S[t][mb]);
+    }
+  }
+  const float sk = a.tscale[2 * u], sv = a.tscale[2 * u + 1];
+  const int live = min(max(nt - 16 * g4, 0), 16);
+  u32x4_t P[NT][2];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+    rows_softmax<NT, true>(st, t, S[t], sk * a.sm_log2e, (1u << live) - 1u, P[t]);
+#pragma unroll
+  for (int cb = 0; cb < 8; ++cb) {
+    const int8_t* vr = a.tv + (u * 128 + 8 * n + cb) * 64 + 16 * g4;
+    f4 acc[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) acc[t] = f4{0, 0, 0, 0};
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const unsigned w0 = reinterpret_cast<const unsigned*>(vr)[2 * ks] ^ 0x80808080u;
+      const unsigned w1 = reinterpret_cast<const unsigned*>(vr)[2 * ks + 1] ^ 0x80808080u;
+      u32x4_t A;
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj)
+        A[jj] = int8_pair(__builtin_amdgcn_perm(w1, w0, 0x0c040c00u + 0x00010001u * jj));
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[t] = mfma_h(A, P[t][ks], acc[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st.o[t][cb][r] = __builtin_fmaf(acc[t][r], sv, st.o[t][cb][r]);
+  }
+}
+
+// ---- 64 drafted nodes ------------------------------------------------------------
+__device__ __forceinline__ bool nonfinite_h2(unsigned x) {
+  return (x & 0x7c00u) == 0x7c00u || (x & 0x7c000000u) == 0x7c000000u;
+}
+
+// Nodes 64 j .. of the sequence's tl; Q in order kOrdNat.  A value that is not
+// finite must not reach the rows that do not see its node (0 * NaN): it takes no
+// part in the products and is added to the rows that do afterwards.
+template <int NT>
+__device__ __forceinline__ void step_nodes(const RowsArgs& a, int b, long u, int j, int tl,
+                                           const RowsQ<NT>& Q, RowsState<NT>& st) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
+  const unsigned short* kb = a.kt + u * a.T * 128;
+  const unsigned short* vb = a.vt + u * a.T * 128;
+  f4 S[NT][4];
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb) {
+    const int tok = 64 * j + 16 * (n >> 2) + 4 * mb + (n & 3);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) S[t][mb] = f4{0, 0, 0, 0};
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      u4_any A = {0, 0, 0, 0};
+      if (tok < tl) A = reinterpret_cast<const u4_any*>(kb + (long)tok * 128 + 32 * g4)[ks];
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        S[t][mb] = mfma_h(u32x4_t{A.x, A.y, A.z, A.w}, Q.x[t][ks], S[t][mb]);
+    }
+  }
+  const int live = min(max(tl - 64 * j - 16 * g4, 0), 16);
+  u32x4_t P[NT][2];
+  unsigned vis[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    unsigned long long w = 0;
+    if (Q.at[t] >= 0) {
+      if (a.mask) {
+        w = a.mask[((long)b * a.T + Q.node[t]) * a.mwords + j];
+      } else {
+        const int c = Q.node[t] + 1 - 64 * j;  // nodes of this tile up to the row's own
+        w = c >= 64 ? ~0ull : (c > 0 ? (1ull << c) - 1ull : 0ull);
+      }
+    }
+    vis[t] = (unsigned)(w >> (16 * g4)) & ((1u << live) - 1u);
+    rows_softmax<NT, true>(st, t, S[t], a.sm_log2e, vis[t], P[t]);
+  }
+  f4 acc[NT][8];
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb) acc[t][cb] = f4{0, 0, 0, 0};
+  bool bad = false;
+#pragma unroll
+  for (int ks = 0; ks < 2; ++ks) {
+    unsigned v[8][4];  // token 8 ks + i of the page, channels 8 n .. 8 n + 7
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int tok = 64 * j + 16 * g4 + 8 * ks + i;
+      u4_any x = {0, 0, 0, 0};
+      if (tok < tl) x = *reinterpret_cast<const u4_any*>(vb + (long)tok * 128 + 8 * n);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        bad = bad || nonfinite_h2(x[e]);
+        v[i][e] = x[e];
+      }
+    }
+    if (__any(bad)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if ((v[i][e] & 0x7c00u) == 0x7c00u) v[i][e] &= 0xffff0000u;
+          if ((v[i][e] & 0x7c000000u) == 0x7c000000u) v[i][e] &= 0xffffu;
+        }
+    }
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb) {
+      u32x4_t A;
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj)
+        A[jj] = __builtin_amdgcn_perm(v[jj + 4][cb >> 1], v[jj][cb >> 1],
+                                      cb & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) acc[t][cb] = mfma_h(A, P[t][ks], acc[t][cb]);
+    }
+  }
+  if (__any(bad)) {
+    const int cnt = min(tl - 64 * j, 64);
+    for (int i = 0; i < cnt; ++i) {
+      const unsigned short* vr = vb + (64L * j + i) * 128 + 32 * g4;
+      const int from = 16 * (i >> 4) + n;  // lane that holds the row's p of token i
+      const int reg = i & 15;              // P[t][ks][jj]: ks = reg >> 3, jj = reg & 3
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        unsigned w = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          w = ((reg >> 3) * 4 + (reg & 3)) == k ? P[t][k >> 2][k & 3] : w;
+        if (reg & 4) w >>= 16;
+        const unsigned pw = __shfl((int)(w & 0xffffu), from);
+        const unsigned seen = __shfl((int)vis[t], from) >> (i & 15);
+        const float p = (float)__builtin_bit_cast(_Float16, (unsigned short)pw);
+        if (!(seen & 1u)) continue;
+#pragma unroll
+        for (int cb = 0; cb < 8; ++cb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const unsigned short x = vr[8 * r + cb];
+            if ((x & 0x7c00u) == 0x7c00u) acc[t][cb][r] += p * (float)__builtin_bit_cast(_Float16, x);
+          }
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb) st.o[t][cb] += acc[t][cb];
+}
+
+// Row `at` of o and lse from its merged state (8 channels from c0).
+__device__ __forceinline__ void rows_store(const RowsArgs& a, long at, int c0, float m, float l,
+                                           const float (&o)[8]) {
+  const bool none = l == 0.0f;  // no visible token
+  const float inv = none ? 0.0f : 1.0f / l;
+  u4_any y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = h2_of(o[2 * e] * inv, o[2 * e + 1] * inv);
+  *reinterpret_cast<u4_any*>(a.o + at * 128 + c0) = y;
+  constexpr float kLn2 = 0x1.62e430p-1f;
+  if (a.lse && c0 == 0) a.lse[at] = none ? -INFINITY : (m + (__builtin_log2f(l) - kPShift)) * kLn2;
+}
+
+// ---- the kernel ------------------------------------------------------------------
+constexpr int kRowsLds = 132;  // floats of a row's state in LDS
+
+template <int BITS, int NT>
+__device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int head_off,
+                                           const RowsSeq& sq, int j0, int j1, RowsQ<NT>& Q,
+                                           RowsState<NT>& st, uint2* szk) {
+  const int w = threadIdx.x >> 6;
+  const long u = (long)b * a.Hkv + kh;
+  int j = j0 + w;
+  if (j < min(j1, sq.nlist)) {
+    load_q<NT, BITS == 4 ? kOrd4 : kOrd2>(a, Q);
+    for (; j < min(j1, sq.nlist); j += kRowsWaves) {
+      const int g = a.sel ? a.sel[u * a.nsel + j] : j;
+      if (g < 0 || g >= sq.ng) continue;
+      RowsGroup<BITS> x;
+      load_group<BITS>(a, b, kh, head_off, g, x);
+      if (x.ok) step_group<BITS, NT>(a, x, Q, st, szk);
+    }
+  }
+  if (j < j1 && j == sq.nlist && sq.nt > 0) {
+    load_q<NT, kOrd4>(a, Q);
+    step_buffer<NT>(a, u, sq.nt, Q, st);
+    j += kRowsWaves;
+  }
+  if (j < j1) {
+    load_q<NT, kOrdNat>(a, Q);
+    for (; j < j1; j += kRowsWaves)
+      step_nodes<NT>(a, b, u, j - sq.nlist - (sq.nt > 0), sq.tl, Q, st);
+  }
+}
+
+template <int NT>
+__global__ __launch_bounds__(64 * kRowsWaves) void k_attn_rows(RowsArgs a) {
+  __shared__ __attribute__((aligned(16))) float part[kRowsWaves][16 * NT][kRowsLds];
+  __shared__ uint2 szk[kRowsWaves][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g4 = lane >> 4;
+  int u = blockIdx.x;
+  const int rt = u % a.ntiles_row;
+  u /= a.ntiles_row;
+  const int s = u % a.nchunk;
+  u /= a.nchunk;
+  const int b = u / a.Hkv, kh = u - b * a.Hkv;
+  const RowsSeq sq = rows_seq(a, b);
+  const int base = 16 * NT * rt, rows = a.G * sq.tl;
+  if (base >= rows || s >= max(sq.nparts, 1)) return;
+  RowsQ<NT> Q;
+  RowsState<NT> st;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int row = base + 16 * t + n;
+    const int h = row / sq.tl;
+    Q.node[t] = row - h * sq.tl;
+    Q.at[t] = row < rows ? ((long)b * a.Hq + kh * a.G + h) * a.T + Q.node[t] : -1;
+    st.m[t] = -INFINITY;
+    st.l[t] = 0.0f;
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb) st.o[t][cb] = f4{0, 0, 0, 0};
+  }
+  const int head_off = 512 * (4 * kh - 2 * __popcll(a.int2_mask & ((1ull << kh) - 1ull)));
+  const int j0 = s * sq.len, j1 = min(j0 + sq.len, sq.ntile);
+  if ((a.int2_mask >> kh) & 1ull)
+    rows_tiles<2, NT>(a, b, kh, head_off, sq, j0, j1, Q, st, szk[w]);
+  else
+    rows_tiles<4, NT>(a, b, kh, head_off, sq, j0, j1, Q, st, szk[w]);
+  // the waves' states to LDS, and their merge
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const float l = add_xor32(st.l[t] + __shfl_xor(st.l[t], 16));
+    float* p = part[w][16 * t + n];
+    if (g4 == 0) *reinterpret_cast<float2*>(p) = make_float2(st.m[t], l);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float* d = p + 4 + 32 * g4 + 8 * r;
+      *reinterpret_cast<f4*>(d) = f4{st.o[t][0][r], st.o[t][1][r], st.o[t][2][r], st.o[t][3][r]};
+      *reinterpret_cast<f4*>(d + 4) = f4{st.o[t][4][r], st.o[t][5][r], st.o[t][6][r], st.o[t][7][r]};
+    }
+  }
+  __syncthreads();
+  const int c0 = 8 * (threadIdx.x & 15);
+  for (int row = threadIdx.x >> 4; row < 16 * NT; row += 4 * kRowsWaves) {
+    if (base + row >= rows) break;
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kRowsWaves; ++i) m = fmaxf(m, part[i][row][0]);
+    float l = 0.0f, o[8] = {};
+#pragma unroll
+    for (int i = 0; i < kRowsWaves; ++i) {
+      const float* p = part[i][row];
+      const float f = p[0] == m ? 1.0f : __builtin_amdgcn_exp2f(p[0] - m);
+      l = __builtin_fmaf(f, p[1], l);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(f, p[4 + c0 + e], o[e]);
+    }
+    const int h = (base + row) / sq.tl;
+    const long at = ((long)b * a.Hq + kh * a.G + h) * a.T + (base + row - h * sq.tl);
+    if (sq.nparts <= 1) {
+      rows_store(a, at, c0, m, l, o);
+    } else {
+      float* p = a.ws + (at * a.nchunk + s) * kWsStride;
+      *reinterpret_cast<float4*>(p + kWsO + c0) = make_float4(o[0], o[1], o[2], o[3]);
+      *reinterpret_cast<float4*>(p + kWsO + c0 + 4) = make_float4(o[4], o[5], o[6], o[7]);
+      if (c0 == 0) *reinterpret_cast<float2*>(p) = make_float2(m, l);
+    }
+  }
+}
+
+// Rows of several chunks: 16 lanes merge a row's states, in the order of the chunks.
+__global__ __launch_bounds__(256) void k_rows_merge(RowsArgs a) {
+  const long at = (long)blockIdx.x * 16 + (threadIdx.x >> 4);
+  if (at >= (long)a.B * a.Hq * a.T) return;
+  const int c0 = 8 * (threadIdx.x & 15);
+  const long bh = at / a.T;
+  const int b = (int)(bh / a.Hq);
+  const RowsSeq sq = rows_seq(a, b);
+  if (at - bh * a.T >= sq.tl || sq.nparts <= 1) return;
+  const float* p = a.ws + at * a.nchunk * kWsStride;
+  float m = -INFINITY;
+  for (int i = 0; i < sq.nparts; ++i) m = fmaxf(m, p[(long)i * kWsStride]);
+  float l = 0.0f, o[8] = {};
+  for (int i = 0; i < sq.nparts; ++i, p += kWsStride) {
+    const float f = p[0] == m ? 1.0f : __builtin_amdgcn_exp2f(p[0] - m);
+    l = __builtin_fmaf(f, p[1], l);
+    const float4 x = *reinterpret_cast<const float4*>(p + kWsO + c0);
+    const float4 y = *reinterpret_cast<const float4*>(p + kWsO + c0 + 4);
+    const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(f, v[e], o[e]);
+  }
+  rows_store(a, at, c0, m, l, o);
+}
+
+// Query rows of a tile of 16 per wave; a work-group covers 16 rows.
+constexpr int kRowsTile = 16;
+
+inline int rows_tiles_per_head(int G, int T) { return ceil_div(G * T, kRowsTile); }
+
+// Chunks of the grid: as many as give the GPU two work-groups per CU, each with at
+// least one tile per wave.
+inline int rows_chunks(int B, int Hkv, int G, int T, int max_tiles) {
+  const long units = (long)B * Hkv * rows_tiles_per_head(G, T);
+  const long want = (512 + units - 1) / units;
+  const long most = ceil_div(max_tiles, kRowsWaves);
+  return (int)(want < most ? (want > 1 ? want : 1) : (most > 1 ? most : 1));
+}
+
+inline hipError_t launch_attn_rows(const RowsArgs& a, hipStream_t stream) {
+  const long groups = (long)a.B * a.Hkv * a.ntiles_row * a.nchunk;
+  hipLaunchKernelGGL((k_attn_rows<1>), dim3((unsigned)groups), dim3(64 * kRowsWaves), 0, stream, a);
+  if (a.nchunk > 1) {
+    const long rows = (long)a.B * a.Hq * a.T;
+    hipLaunchKernelGGL(k_rows_merge, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace turbo

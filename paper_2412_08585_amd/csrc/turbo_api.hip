@@ -14,6 +14,9 @@
 #include "attn_decode.hip"
 #include "head_priority.hip"
 #include "kv_tail.hip"
+#include "attn_rows.hip"
+#include "group_select.hip"
+#include "draft_tree.hip"
 #include "sas_softmax.hip"
 #include "qkv_project.h"
 #include "probes.hip"
@@ -607,6 +610,237 @@ int turbo_append_kv(const void* k_new, const void* v_new, int B, int Hkv, int d,
   a.group_table = group_table;
   a.max_groups = max_groups_per_seq;
   return turbo::launch_append_kv(a, B, stream) == hipSuccess ? TURBO_OK : TURBO_ERR_HIP;
+}
+
+size_t turbo_select_workspace_bytes(int B, int Hq, int max_groups_per_seq) {
+  if (B < 1 || Hq < 1 || max_groups_per_seq < 1) return 0;
+  return (size_t)B * Hq * max_groups_per_seq * sizeof(float);
+}
+
+int turbo_select_groups(const void* q, const turbo_kv_cache* cache, const int32_t* seq_lens,
+                        const int32_t* block_table, const int32_t* group_table,
+                        int max_groups_per_seq, int B, int Hq, int num_select, int keep_first,
+                        int keep_last, void* workspace, size_t workspace_bytes, int32_t* selected,
+                        hipStream_t stream) {
+  if (B < 0 || Hq < 1 || max_groups_per_seq < 1 || !cache || num_select < 1 || keep_first < 0 ||
+      keep_last < 0 || keep_first > num_select || keep_last > num_select - keep_first)
+    return TURBO_ERR_INVALID_ARG;
+  const int Hkv = cache->num_kv_heads;
+  if (Hkv < 1 || Hkv > TURBO_MAX_KV_HEADS || Hq % Hkv != 0 || Hq / Hkv > TURBO_MAX_GQA)
+    return TURBO_ERR_INVALID_ARG;
+  if (B == 0) return TURBO_OK;
+  if (!q || !seq_lens || !block_table || !group_table || !selected) return TURBO_ERR_INVALID_ARG;
+  turbo::SelectArgs a{};
+  int page_bytes = 0;
+  int st = check_cache(cache, Hkv, &a.int2_mask, &page_bytes);
+  if (st != TURBO_OK) return st;
+  if ((long)B * Hkv * turbo::ceil_div(max_groups_per_seq, turbo::kBoundGroups) > 0x7fffffffL)
+    return TURBO_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < turbo_select_workspace_bytes(B, Hq, max_groups_per_seq))
+    return TURBO_ERR_WORKSPACE_TOO_SMALL;
+  st = check_device();
+  if (st != TURBO_OK) return st;
+  a.q = static_cast<const unsigned short*>(q);
+  a.gmeta = cache->group_meta;
+  a.gscale = cache->group_scale;
+  a.npages = (int)std::min<long>(cache->num_pages, 0x7fffffffL);
+  a.nslots = (int)std::min<long>(cache->num_group_slots, 0x7fffffffL);
+  a.seq_lens = seq_lens;
+  a.block_table = block_table;
+  a.group_table = group_table;
+  a.max_groups = max_groups_per_seq;
+  a.B = B;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.G = Hq / Hkv;
+  a.nsel = num_select;
+  a.first = keep_first;
+  a.last = keep_last;
+  a.ws = static_cast<float*>(workspace);
+  a.sel = selected;
+  return turbo::launch_select_groups(a, stream) == hipSuccess ? TURBO_OK : TURBO_ERR_HIP;
+}
+
+// Tiles of 64 tokens the longest sequence can have, and the workspace for them.
+static size_t rows_workspace(int B, int Hq, int Hkv, int T, long tiles) {
+  if (tiles > 0x7fffffffL) return 0;
+  const int n = turbo::rows_chunks(B, Hkv, Hq / Hkv, T, (int)tiles);
+  return n > 1 ? (size_t)B * Hq * T * n * turbo::kWsStride * sizeof(float) : 0;
+}
+
+size_t turbo_selected_workspace_bytes(int B, int Hq, int Hkv, int num_select, int with_tail) {
+  if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || num_select < 1) return 0;
+  return rows_workspace(B, Hq, Hkv, 1, (long)num_select + (with_tail ? 1 : 0));
+}
+
+size_t turbo_tree_workspace_bytes(int B, int Hq, int Hkv, int T, int max_groups_per_seq,
+                                  int with_tail) {
+  if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || T < 1 || T > TURBO_MAX_TREE ||
+      max_groups_per_seq < 1)
+    return 0;
+  return rows_workspace(B, Hq, Hkv, T,
+                        (long)max_groups_per_seq + (with_tail ? 1 : 0) + turbo::ceil_div(T, 64));
+}
+
+// The part turbo_attn_selected and turbo_attn_tree share: a holds what is theirs
+// alone (q, o, lse, and nodes or choice), T rows per query head, at most `tiles` tiles.
+static int attn_rows_impl(turbo::RowsArgs& a, const turbo_kv_cache* cache,
+                          const turbo_kv_tail* tail, const int32_t* seq_lens,
+                          const int32_t* block_table, const int32_t* group_table,
+                          int max_groups_per_seq, int B, int Hq, int T, float sm_scale, long tiles,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const int Hkv = cache->num_kv_heads;
+  int st = check_cache(cache, Hkv, &a.int2_mask, &a.page_bytes);
+  if (st != TURBO_OK) return st;
+  st = check_tail(tail, B, Hkv);
+  if (st != TURBO_OK) return st;
+  if (tiles > 0x7fffffffL || (long)B * Hq * T > 0x7fffffffL) return TURBO_ERR_INVALID_ARG;
+  a.T = T;
+  a.G = Hq / Hkv;
+  a.ntiles_row = turbo::rows_tiles_per_head(a.G, T);
+  a.nchunk = turbo::rows_chunks(B, Hkv, a.G, T, (int)tiles);
+  if ((long)B * Hkv * a.ntiles_row * a.nchunk > 0x7fffffffL) return TURBO_ERR_INVALID_ARG;
+  const size_t need = rows_workspace(B, Hq, Hkv, T, tiles);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return TURBO_ERR_WORKSPACE_TOO_SMALL;
+  st = check_device();
+  if (st != TURBO_OK) return st;
+  a.pages = cache->pages;
+  a.gmeta = cache->group_meta;
+  a.gscale = cache->group_scale;
+  a.npages = (int)std::min<long>(cache->num_pages, 0x7fffffffL);
+  a.nslots = (int)std::min<long>(cache->num_group_slots, 0x7fffffffL);
+  a.seq_lens = seq_lens;
+  a.block_table = block_table;
+  a.group_table = group_table;
+  a.max_groups = max_groups_per_seq;
+  a.B = B;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.sm_log2e = (float)(sm_scale * 1.4426950408889634);
+  if (tail) {
+    a.tk = tail->k;
+    a.tv = tail->v;
+    a.tscale = tail->scale;
+  }
+  a.ws = static_cast<float*>(workspace);
+  return turbo::launch_attn_rows(a, stream) == hipSuccess ? TURBO_OK : TURBO_ERR_HIP;
+}
+
+static bool rows_heads_ok(const turbo_kv_cache* cache, int B, int Hq, int max_groups_per_seq,
+                          float sm_scale) {
+  if (!cache || B < 0 || Hq < 1 || max_groups_per_seq < 1 || !(sm_scale > 0.0f) ||
+      sm_scale > 2.0e38f)
+    return false;
+  const int Hkv = cache->num_kv_heads;
+  return Hkv >= 1 && Hkv <= TURBO_MAX_KV_HEADS && Hq % Hkv == 0 && Hq / Hkv <= TURBO_MAX_GQA;
+}
+
+int turbo_attn_selected(const void* q, const turbo_kv_cache* cache, const turbo_kv_tail* tail,
+                        const int32_t* seq_lens, const int32_t* block_table,
+                        const int32_t* group_table, int max_groups_per_seq,
+                        const int32_t* selected, int num_select, int B, int Hq, float sm_scale,
+                        void* workspace, size_t workspace_bytes, void* o, float* lse,
+                        hipStream_t stream) {
+  if (!rows_heads_ok(cache, B, Hq, max_groups_per_seq, sm_scale) || num_select < 1)
+    return TURBO_ERR_INVALID_ARG;
+  if (B == 0) return TURBO_OK;
+  if (!q || !seq_lens || !block_table || !group_table || !selected || !o)
+    return TURBO_ERR_INVALID_ARG;
+  turbo::RowsArgs a{};
+  a.q = static_cast<const unsigned short*>(q);
+  a.sel = selected;
+  a.nsel = num_select;
+  a.o = static_cast<unsigned short*>(o);
+  a.lse = lse;
+  return attn_rows_impl(a, cache, tail, seq_lens, block_table, group_table, max_groups_per_seq, B,
+                        Hq, 1, sm_scale, (long)num_select + (tail ? 1 : 0), workspace,
+                        workspace_bytes, stream);
+}
+
+int turbo_tree_mask(const int32_t* parents, const int32_t* tree_lens, int B, int T, uint64_t* mask,
+                    int32_t* depth, hipStream_t stream) {
+  if (B < 0 || T < 1 || T > TURBO_MAX_TREE) return TURBO_ERR_INVALID_ARG;
+  if (B == 0) return TURBO_OK;
+  if (!parents || !tree_lens || !mask) return TURBO_ERR_INVALID_ARG;
+  const int st = check_device();
+  if (st != TURBO_OK) return st;
+  turbo::TreeMaskArgs a{};
+  a.parents = parents;
+  a.tree_lens = tree_lens;
+  a.T = T;
+  a.words = turbo::ceil_div(T, 64);
+  a.mask = reinterpret_cast<unsigned long long*>(mask);
+  a.depth = depth;
+  return turbo::launch_tree_mask(a, B, stream) == hipSuccess ? TURBO_OK : TURBO_ERR_HIP;
+}
+
+int turbo_attn_tree(const void* q, const void* k_tree, const void* v_tree,
+                    const uint64_t* tree_mask, const int32_t* tree_lens,
+                    const turbo_kv_cache* cache, const turbo_kv_tail* tail,
+                    const int32_t* seq_lens, const int32_t* block_table,
+                    const int32_t* group_table, int max_groups_per_seq, int B, int Hq, int T,
+                    float sm_scale, void* workspace, size_t workspace_bytes, void* o, float* lse,
+                    hipStream_t stream) {
+  if (!rows_heads_ok(cache, B, Hq, max_groups_per_seq, sm_scale) || T < 1 || T > TURBO_MAX_TREE)
+    return TURBO_ERR_INVALID_ARG;
+  if (B == 0) return TURBO_OK;
+  if (!q || !k_tree || !v_tree || !tree_lens || !seq_lens || !block_table || !group_table || !o)
+    return TURBO_ERR_INVALID_ARG;
+  turbo::RowsArgs a{};
+  a.q = static_cast<const unsigned short*>(q);
+  a.kt = static_cast<const unsigned short*>(k_tree);
+  a.vt = static_cast<const unsigned short*>(v_tree);
+  a.mask = reinterpret_cast<const unsigned long long*>(tree_mask);
+  a.mwords = turbo::ceil_div(T, 64);
+  a.tree_lens = tree_lens;
+  a.o = static_cast<unsigned short*>(o);
+  a.lse = lse;
+  return attn_rows_impl(a, cache, tail, seq_lens, block_table, group_table, max_groups_per_seq, B,
+                        Hq, T, sm_scale,
+                        (long)max_groups_per_seq + (tail ? 1 : 0) + turbo::ceil_div(T, 64),
+                        workspace, workspace_bytes, stream);
+}
+
+int turbo_append_path(const void* k_tree, const void* v_tree, int B, int Hkv, int T, int d,
+                      const int32_t* path, const int32_t* path_lens, int max_path,
+                      const int32_t* seq_lens, const turbo_kv_cache* cache,
+                      const turbo_kv_tail* tail, const int32_t* block_table,
+                      const int32_t* group_table, int max_groups_per_seq, hipStream_t stream) {
+  if (B < 0 || Hkv < 1 || Hkv > TURBO_MAX_KV_HEADS || T < 1 || T > TURBO_MAX_TREE ||
+      d != TURBO_HEAD_DIM || max_path < 1 || max_groups_per_seq < 1)
+    return TURBO_ERR_INVALID_ARG;
+  if (B == 0) return TURBO_OK;
+  if (!k_tree || !v_tree || !path || !path_lens || !seq_lens || !cache || !tail || !block_table ||
+      !group_table)
+    return TURBO_ERR_INVALID_ARG;
+  if ((long)B * Hkv > 0x7fffffffL) return TURBO_ERR_INVALID_ARG;
+  turbo::AppendPathArgs a{};
+  int st = check_cache(cache, Hkv, &a.c.int2_mask, &a.c.page_bytes);
+  if (st != TURBO_OK) return st;
+  st = check_tail(tail, B, Hkv);
+  if (st != TURBO_OK) return st;
+  st = check_device();
+  if (st != TURBO_OK) return st;
+  a.kt = static_cast<const unsigned short*>(k_tree);
+  a.vt = static_cast<const unsigned short*>(v_tree);
+  a.path = path;
+  a.path_lens = path_lens;
+  a.T = T;
+  a.max_path = max_path;
+  a.c.seq_lens = seq_lens;
+  a.c.Hkv = Hkv;
+  a.c.tk = tail->k;
+  a.c.tv = tail->v;
+  a.c.tscale = tail->scale;
+  a.c.pages = cache->pages;
+  a.c.gmeta = cache->group_meta;
+  a.c.gscale = cache->group_scale;
+  a.c.num_pages = cache->num_pages;
+  a.c.num_slots = cache->num_group_slots;
+  a.c.block_table = block_table;
+  a.c.group_table = group_table;
+  a.c.max_groups = max_groups_per_seq;
+  return turbo::launch_append_path(a, B, stream) == hipSuccess ? TURBO_OK : TURBO_ERR_HIP;
 }
 
 int turbo_probe_mfma_i8(int iters, int* sink, int64_t* ops, hipStream_t stream) {
