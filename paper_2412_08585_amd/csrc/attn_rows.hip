@@ -8,11 +8,16 @@
 // cached group, code * s for the buffer, fp16 for a drafted node.  One pass over
 // the tokens in tiles of 64 with the running maximum m and sum l of each row,
 // everything in binary32 but the operands of the matrix instructions:
-//  * K and V as fp16 integers code * s^int + z^int (|.| <= 2048: exact), q as
-//    given: the products of Q K^T are exact, their sums binary32;
-//  * P = 2^(x - m + 15), rounded to fp16 (relative 2^-11, as the output's own
-//    rounding); the 2^15 keeps terms down to 2^-29 of the row's largest in fp16's
-//    normal range.  l sums P before it is rounded.
+//  * K and V as fp16 integers code * s^int + z^int times a power of two (exact), q
+//    as given: the products of Q K^T are exact, their sums binary32;
+//  * the weights P, rounded to fp16 (relative 2^-11, as the output's own rounding).
+// The scale of a tile's V goes into its weights, so that the products of all tiles
+// add up in the accumulators with no pass over them in between: with e = log2 of the
+// tile's scale (x in units of log2 from here on)
+//   P_t = 2^(x_t + e - m + 7),  O += P V,  l += 2^-e sum_t P_t,  m ~ max (x_t + e),
+// o = O / l.  m follows the maximum only when it is more than 8 behind (the row's
+// sums are then rescaled), so 2^7 leaves P below 2^15 and terms down to 2^-21 of the
+// row's largest in fp16's normal range.  l sums P before it is rounded.
 //
 // The tokens of the G query heads of a KV head are one matrix of G * T rows.  A
 // wave takes 16 of them and a tile:
@@ -66,7 +71,7 @@ struct RowsArgs {
 };
 
 constexpr int kRowsWaves = 4;   // waves of a work-group, a tile each in turn
-constexpr float kPShift = 15.0f;
+constexpr float kPShift = 7.0f;
 
 // The tiles of sequence b: cached groups (or choices), the buffer, the nodes.
 struct RowsSeq {
@@ -105,33 +110,58 @@ __device__ __forceinline__ unsigned h2_fma(unsigned a, unsigned b, unsigned c) {
 __device__ __forceinline__ unsigned h2_add(unsigned a, unsigned b) {
   return __builtin_bit_cast(unsigned, __builtin_bit_cast(h2, a) + __builtin_bit_cast(h2, b));
 }
+__device__ __forceinline__ unsigned h2_mul(unsigned a, unsigned b) {
+  return __builtin_bit_cast(unsigned, __builtin_bit_cast(h2, a) * __builtin_bit_cast(h2, b));
+}
 __device__ __forceinline__ unsigned h2_of(float lo, float hi) {
   const h2 x = {(_Float16)lo, (_Float16)hi};
   return __builtin_bit_cast(unsigned, x);
 }
 
-// Codes to fp16.  Pair i of a word (int4: nibbles i, i + 4; int2: fields i, i + 8)
-// goes to the top mantissa bits of the two halves of 1.0: 1 + code / 2^bits.  With
-// s' = 2^bits s and z' = z - 2^bits s, fma(1 + code / 2^bits, s', z') = code s + z,
-// an integer: exact while s' + |z| <= 2048, as in every group this library writes
-// (s <= 16 with 4 bits, 80 with 2).
+// Codes to fp16.  A field of a half's low bits, masked, is the subnormal number
+// field * 2^-24, and one fused multiply-add by a power of two times s^int and to
+// z^int makes of it (code s + z) 2^-kDown, exactly: no conversion.  Pair i of a word
+// (int4: nibbles i and i + 4; int2: fields i and i + 8) is brought to the lowest or
+// second lowest field of its half, whose factors differ by 2^bits: a shift for every
+// two pairs.  Exact, and s' finite, for the s^int this library writes (at most 16
+// with 4 bits, 80 with 2).  9 instructions for 8 codes of 4 bits; by way of
+// 1 + code / 16 it takes 12.
+template <int BITS>
+constexpr int kDown = BITS == 4 ? 13 : 15;
+
 template <int BITS>
 __device__ __forceinline__ unsigned code_pair(unsigned w, int i) {
-  constexpr int at = 10 - BITS;  // bit of the field in the half
-  const int sh = BITS * i - at;
-  const unsigned x = sh > 0 ? w >> sh : w << -sh;
-  constexpr unsigned m = BITS == 4 ? 0x03C003C0u : 0x03000300u;
-  return (x & m) | 0x3C003C00u;
+  constexpr unsigned m = BITS == 4 ? 0x000f000fu : 0x00030003u;
+  return (w >> (2 * BITS * (i >> 1))) & (i & 1 ? m << BITS : m);
 }
 
-// s' and z' of two channels, their s^int and z^int bytes in bits 0-7 and 16-23 of
-// s and z.  (0x6400 | x is 1024 + x.)
+// 2^e as fp16 in both halves.
+constexpr unsigned h2_exp2(int e) {  // (subnormal below 2^-14)
+  const unsigned h = e >= -14 ? (unsigned)(15 + e) << 10 : 1u << (24 + e);
+  return h | h << 16;
+}
+
+// s^int and z^int of two channels (bytes at bits 0-7 and 16-23) as fp16 integers.
+// (0x6400 | x is 1024 + x.)
+__device__ __forceinline__ unsigned scale_h2(unsigned s) {
+  return h2_add(s | 0x64006400u, 0xe400e400u);
+}
+__device__ __forceinline__ unsigned zero_h2(unsigned z) {
+  return h2_add((z ^ 0x00800080u) | 0x64006400u, 0xe480e480u);
+}
+// Factors of pairs in the lowest (odd = 0) and second lowest field, and z 2^-kDown.
 template <int BITS>
-__device__ __forceinline__ void scale_pair(unsigned s, unsigned z, unsigned& sp, unsigned& zp) {
-  constexpr float f = 1 << BITS;
-  sp = h2_fma(s | 0x64006400u, h2_of(f, f), h2_of(-1024.0f * f, -1024.0f * f));
-  const unsigned zi = h2_add((z ^ 0x00800080u) | 0x64006400u, h2_of(-1152.0f, -1152.0f));
-  zp = h2_add(zi, sp ^ 0x80008000u);
+__device__ __forceinline__ unsigned scale_at(unsigned s, int odd) {
+  return h2_mul(s, odd ? h2_exp2(24 - kDown<BITS> - BITS) : h2_exp2(24 - kDown<BITS>));
+}
+template <int BITS>
+__device__ __forceinline__ unsigned zero_at(unsigned z) {
+  return h2_mul(z, h2_exp2(-kDown<BITS>));
+}
+__device__ __forceinline__ unsigned h2_splat(unsigned x, int hi) {
+  const h2 v = __builtin_bit_cast(h2, x);
+  const h2 y = hi ? h2{v[1], v[1]} : h2{v[0], v[0]};
+  return __builtin_bit_cast(unsigned, y);
 }
 
 // int8 pair (bytes at bits 0-7 and 16-23, high bits flipped) to fp16.
@@ -192,43 +222,49 @@ struct RowsState {
   float m[NT], l[NT];
 };
 
-// Scores to probabilities: S holds the products of row tile t, x = S * c2; bit
-// 4 mb + r of vis says whether token (mb, r) of the lane's page is visible.  Rescales
-// the state and returns P as the B operand of O^T: PAIR4 pairs tokens (8 ks + jj,
-// + 4) of the page, else (4 ks + jj, + 8).
-template <int NT, bool PAIR4>
-__device__ __forceinline__ void rows_softmax(RowsState<NT>& st, int t, f4 (&S)[4], float c2,
-                                             unsigned vis, u32x4_t (&P)[2]) {
+// Scores of a tile to weights.  S holds the products of row tile t, x = S * c2; ex
+// and inv are log2 of the scale of the tile's V and its inverse; where MASKED, bit
+// 4 mb + r of vis says whether token (mb, r) of the lane's page is visible.  Brings
+// the state to the tile's maximum and returns P as the B operand of O^T: PAIR4 pairs
+// tokens (8 ks + jj, + 4) of the page, else (4 ks + jj, + 8).
+template <int NT, bool PAIR4, bool MASKED>
+__device__ __forceinline__ void rows_softmax(RowsState<NT>& st, int t, f4 (&S)[4], float c2, float ex,
+                                             float inv, unsigned vis, u32x4_t (&P)[2]) {
+  if (MASKED) {
 #pragma unroll
-  for (int mb = 0; mb < 4; ++mb)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const float x = S[mb][r] * c2;
-      S[mb][r] = (vis >> (4 * mb + r)) & 1u ? x : -INFINITY;
+    for (int i = 0; i < 16; ++i) {
+      const float x = S[i >> 2][i & 3] * c2;
+      S[i >> 2][i & 3] = (vis >> i) & 1u ? x : -INFINITY;
     }
+    c2 = 1.0f;
+  }
+  // (plain maxima: a matrix result must not be read by inline asm, before which the
+  // compiler inserts no wait states)
   float mx = S[0][0];
 #pragma unroll
   for (int i = 1; i < 16; ++i) mx = fmaxf(mx, S[i >> 2][i & 3]);
-  mx = max_xor32(max_xor16(mx));
-  const float mo = st.m[t], mn = fmaxf(mo, mx);
-  st.m[t] = mn;
-  if (__any(mn != mo)) {
+  mx = __builtin_fmaf(max_xor32_nn(max_xor16_nn(mx)), c2, ex);  // (c2 >= 0)
+  const float mo = st.m[t];
+  const bool up = mx > mo + 8.0f;
+  if (__any(up)) {
+    const float mn = up ? mx : mo;
     // (a row that has seen nothing yet: its sums are zero)
     const float al = mo == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mo - mn);
+    st.m[t] = mn;
     st.l[t] *= al;
 #pragma unroll
     for (int cb = 0; cb < 8; ++cb) st.o[t][cb] *= al;
   }
-  const float off = mn == -INFINITY ? 0.0f : kPShift - mn;
-  float l = 0.0f;
+  const float off = st.m[t] == -INFINITY ? 0.0f : (kPShift + ex) - st.m[t];
+  float l[4] = {};
 #pragma unroll
   for (int mb = 0; mb < 4; ++mb)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      S[mb][r] = __builtin_amdgcn_exp2f(S[mb][r] + off);
-      l += S[mb][r];
+      S[mb][r] = __builtin_amdgcn_exp2f(MASKED ? S[mb][r] + off : __builtin_fmaf(S[mb][r], c2, off));
+      l[r] += S[mb][r];
     }
-  st.l[t] += l;
+  st.l[t] = __builtin_fmaf((l[0] + l[1]) + (l[2] + l[3]), inv, st.l[t]);
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -236,29 +272,80 @@ __device__ __forceinline__ void rows_softmax(RowsState<NT>& st, int t, f4 (&S)[4
       P[ks][jj] = PAIR4 ? h2_of(S[2 * ks][jj], S[2 * ks + 1][jj]) : h2_of(S[ks][jj], S[ks + 2][jj]);
 }
 
+// log2 and inverse of the scale of a tile's V (times 2^down); a scale of zero has
+// only zeros behind it and counts as one.
+__device__ __forceinline__ void value_scale(float sv, float up, float& ex, float& inv) {
+  const float s = sv == 0.0f ? 1.0f : sv * up;
+  ex = __builtin_amdgcn_logf(s);
+  inv = __builtin_amdgcn_rcpf(s);
+}
+
 // ---- a cached group ------------------------------------------------------------
+// Table entries and scales of the wave's next 64 tiles, lane i holding the i-th: one
+// round of loads for 64 steps, and no step waits for a table entry before its codes
+// can leave.
+struct RowsTab {
+  int pg[4];     // pages, 0 where there is nothing to attend
+  int slot;      // -1 where there is nothing to attend
+  float sk, sv;
+};
+
+// Lane i: the tile j + i * kRowsWaves of the list, attended below j1.
+__device__ __forceinline__ void load_tab(const RowsArgs& a, int b, int kh, const RowsSeq& sq, int j,
+                                         int j1, RowsTab& T) {
+  j += (int)(threadIdx.x & 63) * kRowsWaves;
+  bool ok = j < j1;
+  int g = ok ? j : 0;
+  if (a.sel) g = ok ? a.sel[((long)b * a.Hkv + kh) * a.nsel + j] : 0;
+  ok = ok && g >= 0 && g < sq.ng;
+  T.slot = -1;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) T.pg[i] = 0;
+  T.sk = T.sv = 0.0f;
+  if (ok) {
+    const int* bt = a.block_table + ((long)b * a.max_groups + g) * 4;
+    const int slot = a.group_table[(long)b * a.max_groups + g];
+    int pg[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      pg[i] = bt[i];
+      ok = ok && pg[i] >= 0 && pg[i] < a.npages;
+    }
+    if (ok && slot >= 0 && slot < a.nslots) {
+      T.slot = slot;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) T.pg[i] = pg[i];
+      const float* gs = a.gscale + ((long)slot * a.Hkv + kh) * 2;
+      T.sk = gs[0];
+      T.sv = gs[1];
+    }
+  }
+}
+
+// Codes and metadata of a group, loaded a step ahead.
 template <int BITS>
 struct RowsGroup {
-  bool ok;
   unsigned k[4][BITS];     // codes of token (m, mb), the lane's 32 channels
   unsigned v[8 * BITS / 2];  // codes of channels 8 n .. 8 n + 7, the lane's page
   uint2 ks, kz;            // s^int, z^int of the 8 channels that hold the lane's pair
   uint2 vs, vz;            // of channels 8 n .. 8 n + 7
-  float sk, sv;
 };
 
+// The i-th tile of T.  One with nothing to attend loads page 0 and slot 0, so that
+// as many loads are in flight on every path.
 template <int BITS>
-__device__ __forceinline__ void load_group(const RowsArgs& a, int b, int kh, int head_off, int g,
-                                           RowsGroup<BITS>& x) {
+__device__ __forceinline__ void load_group(const RowsArgs& a, int kh, int head_off, const RowsTab& T,
+                                           int i, RowsGroup<BITS>& x) {
   const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
-  const int* bt = a.block_table + (long)b * 4 * a.max_groups + 4L * g;
-  const int slot = a.group_table[(long)b * a.max_groups + g];
-  bool ok = slot >= 0 && slot < a.nslots;
+  int pg[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) ok = ok && bt[i] >= 0 && bt[i] < a.npages;
-  x.ok = ok;
-  if (!ok) return;  // skipped: nothing of it is read
-  const uint8_t* kp = a.pages + (long)bt[n >> 2] * a.page_bytes + head_off + (n & 3) * 16 * BITS + 4 * BITS * g4;
+  for (int p = 0; p < 4; ++p) pg[p] = __builtin_amdgcn_readlane(T.pg[p], i);
+  const int slot = max(__builtin_amdgcn_readlane(T.slot, i), 0);
+  auto page_of = [&](int p) {
+    const int lo = p & 1 ? pg[1] : pg[0], hi = p & 1 ? pg[3] : pg[2];
+    return (long)(p & 2 ? hi : lo) * a.page_bytes;
+  };
+  const uint8_t* kp = a.pages + page_of(n >> 2) + head_off + (n & 3) * 16 * BITS + 4 * BITS * g4;
 #pragma unroll
   for (int mb = 0; mb < 4; ++mb) {
     if constexpr (BITS == 4) {
@@ -269,12 +356,6 @@ __device__ __forceinline__ void load_group(const RowsArgs& a, int b, int kh, int
       x.k[mb][0] = w.x; x.k[mb][1] = w.y;
     }
   }
-  const uint8_t* vp = a.pages + (long)bt[g4] * a.page_bytes + head_off + 256 * BITS + n * 16 * BITS;
-#pragma unroll
-  for (int i = 0; i < BITS; ++i) {
-    const u32x4_t w = load_nt4(vp + 16 * i);
-    x.v[4 * i] = w.x; x.v[4 * i + 1] = w.y; x.v[4 * i + 2] = w.z; x.v[4 * i + 3] = w.w;
-  }
   const int8_t* meta = a.gmeta + ((long)slot * a.Hkv + kh) * 512;
   // the lane converts pair (ks, jj) = (n >> 2, n & 3) of its channels
   constexpr int ORD = BITS == 4 ? kOrd4 : kOrd2;
@@ -283,25 +364,28 @@ __device__ __forceinline__ void load_group(const RowsArgs& a, int b, int kh, int
                     *reinterpret_cast<const unsigned*>(meta + c + kChanDist<ORD>));
   x.kz = make_uint2(*reinterpret_cast<const unsigned*>(meta + 128 + c),
                     *reinterpret_cast<const unsigned*>(meta + 128 + c + kChanDist<ORD>));
+  const uint8_t* vp = a.pages + page_of(g4) + head_off + 256 * BITS + n * 16 * BITS;
+#pragma unroll
+  for (int i = 0; i < BITS; ++i) {
+    const u32x4_t w = load_nt4(vp + 16 * i);
+    x.v[4 * i] = w.x; x.v[4 * i + 1] = w.y; x.v[4 * i + 2] = w.z; x.v[4 * i + 3] = w.w;
+  }
   x.vs = *reinterpret_cast<const uint2*>(meta + 256 + 8 * n);
   x.vz = *reinterpret_cast<const uint2*>(meta + 384 + 8 * n);
-  const float* gs = a.gscale + ((long)slot * a.Hkv + kh) * 2;
-  x.sk = gs[0];
-  x.sv = gs[1];
 }
 
 template <int BITS, int NT>
-__device__ __forceinline__ void step_group(const RowsArgs& a, const RowsGroup<BITS>& x,
-                                           const RowsQ<NT>& Q, RowsState<NT>& st, uint2* szk) {
+__device__ __forceinline__ void step_group(const RowsArgs& a, const RowsGroup<BITS>& x, float sk,
+                                           float sv, const RowsQ<NT>& Q, RowsState<NT>& st,
+                                           uint2* szk) {
   const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
-  // s' and z' of the lane group's channel pairs, exchanged through LDS
+  // factors and zero points of the lane group's channel pairs, exchanged through LDS
   {
     const int sh = 8 * (n & 3);
-    unsigned sp, zp;
-    scale_pair<BITS>(((x.ks.x >> sh) & 0xffu) | (((x.ks.y >> sh) & 0xffu) << 16),
-                     ((x.kz.x >> sh) & 0xffu) | (((x.kz.y >> sh) & 0xffu) << 16), sp, zp);
+    const unsigned s = scale_h2(((x.ks.x >> sh) & 0xffu) | (((x.ks.y >> sh) & 0xffu) << 16));
+    const unsigned z = zero_h2(((x.kz.x >> sh) & 0xffu) | (((x.kz.y >> sh) & 0xffu) << 16));
     wave_sync();
-    szk[lane] = make_uint2(sp, zp);
+    szk[lane] = make_uint2(n & 1 ? scale_at<BITS>(s, 1) : scale_at<BITS>(s, 0), zero_at<BITS>(z));
     wave_sync();
   }
   f4 S[NT][4];
@@ -327,35 +411,35 @@ __device__ __forceinline__ void step_group(const RowsArgs& a, const RowsGroup<BI
       for (int t = 0; t < NT; ++t) S[t][mb] = mfma_h(A, Q.x[t][ks], S[t][mb]);
     }
   }
+  constexpr float up = 1 << kDown<BITS>;
+  float ex, inv;
+  value_scale(sv, up, ex, inv);
   u32x4_t P[NT][2];
 #pragma unroll
   for (int t = 0; t < NT; ++t)
-    rows_softmax<NT, BITS == 4>(st, t, S[t], x.sk * a.sm_log2e, 0xffffu, P[t]);
+    rows_softmax<NT, BITS == 4, false>(st, t, S[t], sk * (a.sm_log2e * up), ex, inv, 0, P[t]);
 #pragma unroll
-  for (int cb = 0; cb < 8; ++cb) {
-    const unsigned sel = 0x0c000c00u | (unsigned)(cb & 3) | (unsigned)(cb & 3) << 16;
-    unsigned sp, zp;
-    scale_pair<BITS>(__builtin_amdgcn_perm(0u, cb < 4 ? x.vs.x : x.vs.y, sel),
-                     __builtin_amdgcn_perm(0u, cb < 4 ? x.vz.x : x.vz.y, sel), sp, zp);
-    f4 acc[NT];
+  for (int c2 = 0; c2 < 4; ++c2) {  // channels 8 n + 2 c2 and + 1
+    const unsigned sel = c2 & 1 ? 0x0c030c02u : 0x0c010c00u;
+    const unsigned s = scale_h2(__builtin_amdgcn_perm(0u, c2 < 2 ? x.vs.x : x.vs.y, sel));
+    const unsigned z = zero_h2(__builtin_amdgcn_perm(0u, c2 < 2 ? x.vz.x : x.vz.y, sel));
+    const unsigned s0 = scale_at<BITS>(s, 0), s1 = scale_at<BITS>(s, 1), zd = zero_at<BITS>(z);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = f4{0, 0, 0, 0};
+    for (int hi = 0; hi < 2; ++hi) {
+      const int cb = 2 * c2 + hi;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      u32x4_t A;
+      for (int ks = 0; ks < 2; ++ks) {
+        u32x4_t A;
 #pragma unroll
-      for (int jj = 0; jj < 4; ++jj) {
-        const unsigned c = BITS == 4 ? code_pair<BITS>(x.v[2 * cb + ks], jj)
-                                     : code_pair<BITS>(x.v[cb], 4 * ks + jj);
-        A[jj] = h2_fma(c, sp, zp);
+        for (int jj = 0; jj < 4; ++jj) {
+          const unsigned c = BITS == 4 ? code_pair<BITS>(x.v[2 * cb + ks], jj)
+                                       : code_pair<BITS>(x.v[cb], 4 * ks + jj);
+          A[jj] = h2_fma(c, h2_splat(jj & 1 ? s1 : s0, hi), h2_splat(zd, hi));
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) st.o[t][cb] = mfma_h(A, P[t][ks], st.o[t][cb]);
       }
-#pragma unroll
-      for (int t = 0; t < NT; ++t) acc[t] = mfma_h(A, P[t][ks], acc[t]);
     }
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) st.o[t][cb][r] = __builtin_fmaf(acc[t][r], x.sv, st.o[t][cb][r]);
   }
 }
 
@@ -384,18 +468,17 @@ __device__ __forceinline__ void step_buffer(const RowsArgs& a, long u, int nt, c
       for (int t = 0; t < NT; ++t) S[t][mb] = mfma_h(A, Q.x[t][ks], S[t][mb]);
     }
   }
-  const float sk = a.tscale[2 * u], sv = a.tscale[2 * u + 1];
+  const float sk = a.tscale[2 * u];
+  float ex, inv;
+  value_scale(a.tscale[2 * u + 1], 1.0f, ex, inv);
   const int live = min(max(nt - 16 * g4, 0), 16);
   u32x4_t P[NT][2];
 #pragma unroll
   for (int t = 0; t < NT; ++t)
-    rows_softmax<NT, true>(st, t, S[t], sk * a.sm_log2e, (1u << live) - 1u, P[t]);
+    rows_softmax<NT, true, true>(st, t, S[t], sk * a.sm_log2e, ex, inv, (1u << live) - 1u, P[t]);
 #pragma unroll
   for (int cb = 0; cb < 8; ++cb) {
     const int8_t* vr = a.tv + (u * 128 + 8 * n + cb) * 64 + 16 * g4;
-    f4 acc[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) acc[t] = f4{0, 0, 0, 0};
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       const unsigned w0 = reinterpret_cast<const unsigned*>(vr)[2 * ks] ^ 0x80808080u;
@@ -405,12 +488,8 @@ __device__ __forceinline__ void step_buffer(const RowsArgs& a, long u, int nt, c
       for (int jj = 0; jj < 4; ++jj)
         A[jj] = int8_pair(__builtin_amdgcn_perm(w1, w0, 0x0c040c00u + 0x00010001u * jj));
 #pragma unroll
-      for (int t = 0; t < NT; ++t) acc[t] = mfma_h(A, P[t][ks], acc[t]);
+      for (int t = 0; t < NT; ++t) st.o[t][cb] = mfma_h(A, P[t][ks], st.o[t][cb]);
     }
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) st.o[t][cb][r] = __builtin_fmaf(acc[t][r], sv, st.o[t][cb][r]);
   }
 }
 
@@ -458,13 +537,8 @@ __device__ __forceinline__ void step_nodes(const RowsArgs& a, int b, long u, int
       }
     }
     vis[t] = (unsigned)(w >> (16 * g4)) & ((1u << live) - 1u);
-    rows_softmax<NT, true>(st, t, S[t], a.sm_log2e, vis[t], P[t]);
+    rows_softmax<NT, true, true>(st, t, S[t], a.sm_log2e, 0.0f, 1.0f, vis[t], P[t]);
   }
-  f4 acc[NT][8];
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int cb = 0; cb < 8; ++cb) acc[t][cb] = f4{0, 0, 0, 0};
   bool bad = false;
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) {
@@ -497,7 +571,7 @@ __device__ __forceinline__ void step_nodes(const RowsArgs& a, int b, long u, int
         A[jj] = __builtin_amdgcn_perm(v[jj + 4][cb >> 1], v[jj][cb >> 1],
                                       cb & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-      for (int t = 0; t < NT; ++t) acc[t][cb] = mfma_h(A, P[t][ks], acc[t][cb]);
+      for (int t = 0; t < NT; ++t) st.o[t][cb] = mfma_h(A, P[t][ks], st.o[t][cb]);
     }
   }
   if (__any(bad)) {
@@ -522,15 +596,11 @@ __device__ __forceinline__ void step_nodes(const RowsArgs& a, int b, long u, int
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const unsigned short x = vr[8 * r + cb];
-            if ((x & 0x7c00u) == 0x7c00u) acc[t][cb][r] += p * (float)__builtin_bit_cast(_Float16, x);
+            if ((x & 0x7c00u) == 0x7c00u) st.o[t][cb][r] += p * (float)__builtin_bit_cast(_Float16, x);
           }
       }
     }
   }
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int cb = 0; cb < 8; ++cb) st.o[t][cb] += acc[t][cb];
 }
 
 // Row `at` of o and lse from its merged state (8 channels from c0).
@@ -556,15 +626,27 @@ __device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int
   const int w = threadIdx.x >> 6;
   const long u = (long)b * a.Hkv + kh;
   int j = j0 + w;
-  if (j < min(j1, sq.nlist)) {
+  const int je = min(j1, sq.nlist);
+  if (j < je) {
     load_q<NT, BITS == 4 ? kOrd4 : kOrd2>(a, Q);
-    for (; j < min(j1, sq.nlist); j += kRowsWaves) {
-      const int g = a.sel ? a.sel[u * a.nsel + j] : j;
-      if (g < 0 || g >= sq.ng) continue;
-      RowsGroup<BITS> x;
-      load_group<BITS>(a, b, kh, head_off, g, x);
-      if (x.ok) step_group<BITS, NT>(a, x, Q, st, szk);
+    const int cnt = ceil_div(je - j, kRowsWaves);
+    RowsTab T;
+    load_tab(a, b, kh, sq, j, je, T);
+    RowsGroup<BITS> x[2];
+    load_group<BITS>(a, kh, head_off, T, 0, x[0]);
+    for (int i = 0; i < cnt; i += 2) {
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const int at = (i + p) & 63;
+        const bool live = __builtin_amdgcn_readlane(T.slot, at) >= 0;
+        const float sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sk), at));
+        const float sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sv), at));
+        if (at == 63) load_tab(a, b, kh, sq, j + kRowsWaves * (i + p + 1), je, T);
+        load_group<BITS>(a, kh, head_off, T, (i + p + 1) & 63, x[1 - p]);
+        if (live && i + p < cnt) step_group<BITS, NT>(a, x[p], sk, sv, Q, st, szk);
+      }
     }
+    j += kRowsWaves * cnt;
   }
   if (j < j1 && j == sq.nlist && sq.nt > 0) {
     load_q<NT, kOrd4>(a, Q);
@@ -678,10 +760,9 @@ __global__ __launch_bounds__(256) void k_rows_merge(RowsArgs a) {
   rows_store(a, at, c0, m, l, o);
 }
 
-// Query rows of a tile of 16 per wave; a work-group covers 16 rows.
-constexpr int kRowsTile = 16;
-
-inline int rows_tiles_per_head(int G, int T) { return ceil_div(G * T, kRowsTile); }
+// Tiles of 16 query rows that a wave takes: a second one shares the codes' expansion.
+inline int rows_nt(int G, int T) { return G * T <= 16 ? 1 : 2; }
+inline int rows_tiles_per_head(int G, int T) { return ceil_div(G * T, 16 * rows_nt(G, T)); }
 
 // Chunks of the grid: as many as give the GPU two work-groups per CU, each with at
 // least one tile per wave.
@@ -694,7 +775,10 @@ inline int rows_chunks(int B, int Hkv, int G, int T, int max_tiles) {
 
 inline hipError_t launch_attn_rows(const RowsArgs& a, hipStream_t stream) {
   const long groups = (long)a.B * a.Hkv * a.ntiles_row * a.nchunk;
-  hipLaunchKernelGGL((k_attn_rows<1>), dim3((unsigned)groups), dim3(64 * kRowsWaves), 0, stream, a);
+  if (rows_nt(a.G, a.T) == 1)
+    hipLaunchKernelGGL((k_attn_rows<1>), dim3((unsigned)groups), dim3(64 * kRowsWaves), 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_attn_rows<2>), dim3((unsigned)groups), dim3(64 * kRowsWaves), 0, stream, a);
   if (a.nchunk > 1) {
     const long rows = (long)a.B * a.Hq * a.T;
     hipLaunchKernelGGL(k_rows_merge, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, a);
