@@ -322,7 +322,7 @@ __device__ __forceinline__ void load_tab(const RowsArgs& a, int b, int kh, const
   }
 }
 
-// Codes and metadata of a group, loaded a step ahead.
+// Codes and metadata of a group.
 template <int BITS>
 struct RowsGroup {
   unsigned k[4][BITS];     // codes of token (m, mb), the lane's 32 channels
@@ -331,21 +331,26 @@ struct RowsGroup {
   uint2 vs, vz;            // of channels 8 n .. 8 n + 7
 };
 
-// The i-th tile of T.  One with nothing to attend loads page 0 and slot 0, so that
-// as many loads are in flight on every path.
-template <int BITS>
-__device__ __forceinline__ void load_group(const RowsArgs& a, int kh, int head_off, const RowsTab& T,
-                                           int i, RowsGroup<BITS>& x) {
-  const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
+// K and V of the i-th tile of T.  One with nothing to attend loads page 0 and slot 0,
+// so that as many loads are in flight on every path.
+__device__ __forceinline__ long tab_page(const RowsArgs& a, const RowsTab& T, int i, int p) {
   int pg[4];
 #pragma unroll
-  for (int p = 0; p < 4; ++p) pg[p] = __builtin_amdgcn_readlane(T.pg[p], i);
+  for (int k = 0; k < 4; ++k) pg[k] = __builtin_amdgcn_readlane(T.pg[k], i);
+  const int lo = p & 1 ? pg[1] : pg[0], hi = p & 1 ? pg[3] : pg[2];
+  return (long)(p & 2 ? hi : lo) * a.page_bytes;
+}
+__device__ __forceinline__ const int8_t* tab_meta(const RowsArgs& a, const RowsTab& T, int i, int kh) {
   const int slot = max(__builtin_amdgcn_readlane(T.slot, i), 0);
-  auto page_of = [&](int p) {
-    const int lo = p & 1 ? pg[1] : pg[0], hi = p & 1 ? pg[3] : pg[2];
-    return (long)(p & 2 ? hi : lo) * a.page_bytes;
-  };
-  const uint8_t* kp = a.pages + page_of(n >> 2) + head_off + (n & 3) * 16 * BITS + 4 * BITS * g4;
+  return a.gmeta + ((long)slot * a.Hkv + kh) * 512;
+}
+
+template <int BITS>
+__device__ __forceinline__ void load_group_k(const RowsArgs& a, int kh, int head_off, const RowsTab& T,
+                                             int i, RowsGroup<BITS>& x) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
+  const uint8_t* kp =
+      a.pages + tab_page(a, T, i, n >> 2) + head_off + (n & 3) * 16 * BITS + 4 * BITS * g4;
 #pragma unroll
   for (int mb = 0; mb < 4; ++mb) {
     if constexpr (BITS == 4) {
@@ -356,28 +361,34 @@ __device__ __forceinline__ void load_group(const RowsArgs& a, int kh, int head_o
       x.k[mb][0] = w.x; x.k[mb][1] = w.y;
     }
   }
-  const int8_t* meta = a.gmeta + ((long)slot * a.Hkv + kh) * 512;
   // the lane converts pair (ks, jj) = (n >> 2, n & 3) of its channels
   constexpr int ORD = BITS == 4 ? kOrd4 : kOrd2;
-  const int c = 32 * g4 + (chan_lo<ORD>(n >> 2, n & 3) & ~3);
-  x.ks = make_uint2(*reinterpret_cast<const unsigned*>(meta + c),
-                    *reinterpret_cast<const unsigned*>(meta + c + kChanDist<ORD>));
-  x.kz = make_uint2(*reinterpret_cast<const unsigned*>(meta + 128 + c),
-                    *reinterpret_cast<const unsigned*>(meta + 128 + c + kChanDist<ORD>));
-  const uint8_t* vp = a.pages + page_of(g4) + head_off + 256 * BITS + n * 16 * BITS;
+  const int8_t* meta = tab_meta(a, T, i, kh) + 32 * g4 + (chan_lo<ORD>(n >> 2, n & 3) & ~3);
+  x.ks = make_uint2(*reinterpret_cast<const unsigned*>(meta),
+                    *reinterpret_cast<const unsigned*>(meta + kChanDist<ORD>));
+  x.kz = make_uint2(*reinterpret_cast<const unsigned*>(meta + 128),
+                    *reinterpret_cast<const unsigned*>(meta + 128 + kChanDist<ORD>));
+}
+
+template <int BITS>
+__device__ __forceinline__ void load_group_v(const RowsArgs& a, int kh, int head_off, const RowsTab& T,
+                                             int i, RowsGroup<BITS>& x) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
+  const uint8_t* vp = a.pages + tab_page(a, T, i, g4) + head_off + 256 * BITS + n * 16 * BITS;
 #pragma unroll
-  for (int i = 0; i < BITS; ++i) {
-    const u32x4_t w = load_nt4(vp + 16 * i);
-    x.v[4 * i] = w.x; x.v[4 * i + 1] = w.y; x.v[4 * i + 2] = w.z; x.v[4 * i + 3] = w.w;
+  for (int e = 0; e < BITS; ++e) {
+    const u32x4_t w = load_nt4(vp + 16 * e);
+    x.v[4 * e] = w.x; x.v[4 * e + 1] = w.y; x.v[4 * e + 2] = w.z; x.v[4 * e + 3] = w.w;
   }
+  const int8_t* meta = tab_meta(a, T, i, kh);
   x.vs = *reinterpret_cast<const uint2*>(meta + 256 + 8 * n);
   x.vz = *reinterpret_cast<const uint2*>(meta + 384 + 8 * n);
 }
 
+// S^T = K q^T of a group.
 template <int BITS, int NT>
-__device__ __forceinline__ void step_group(const RowsArgs& a, const RowsGroup<BITS>& x, float sk,
-                                           float sv, const RowsQ<NT>& Q, RowsState<NT>& st,
-                                           uint2* szk) {
+__device__ __forceinline__ void group_scores(const RowsGroup<BITS>& x, const RowsQ<NT>& Q,
+                                             f4 (&S)[NT][4], uint2* szk) {
   const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
   // factors and zero points of the lane group's channel pairs, exchanged through LDS
   {
@@ -388,7 +399,6 @@ __device__ __forceinline__ void step_group(const RowsArgs& a, const RowsGroup<BI
     szk[lane] = make_uint2(n & 1 ? scale_at<BITS>(s, 1) : scale_at<BITS>(s, 0), zero_at<BITS>(z));
     wave_sync();
   }
-  f4 S[NT][4];
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -411,13 +421,12 @@ __device__ __forceinline__ void step_group(const RowsArgs& a, const RowsGroup<BI
       for (int t = 0; t < NT; ++t) S[t][mb] = mfma_h(A, Q.x[t][ks], S[t][mb]);
     }
   }
-  constexpr float up = 1 << kDown<BITS>;
-  float ex, inv;
-  value_scale(sv, up, ex, inv);
-  u32x4_t P[NT][2];
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-    rows_softmax<NT, BITS == 4, false>(st, t, S[t], sk * (a.sm_log2e * up), ex, inv, 0, P[t]);
+}
+
+// O^T += V^T P^T of a group.
+template <int BITS, int NT>
+__device__ __forceinline__ void group_values(const RowsGroup<BITS>& x, const u32x4_t (&P)[NT][2],
+                                             RowsState<NT>& st) {
 #pragma unroll
   for (int c2 = 0; c2 < 4; ++c2) {  // channels 8 n + 2 c2 and + 1
     const unsigned sel = c2 & 1 ? 0x0c030c02u : 0x0c010c00u;
@@ -616,6 +625,18 @@ __device__ __forceinline__ void rows_store(const RowsArgs& a, long at, int c0, f
   if (a.lse && c0 == 0) a.lse[at] = none ? -INFINITY : (m + (__builtin_log2f(l) - kPShift)) * kLn2;
 }
 
+// (m, l, o) and another state of the same row.
+__device__ __forceinline__ void rows_join(float& m, float& l, float (&o)[8], float pm, float pl,
+                                          const float (&v)[8]) {
+  const float mn = fmaxf(m, pm);
+  const float f = m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+  const float g = pm == mn ? 1.0f : __builtin_amdgcn_exp2f(pm - mn);
+  m = mn;
+  l = __builtin_fmaf(g, pl, f * l);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(g, v[e], f * o[e]);
+}
+
 // ---- the kernel ------------------------------------------------------------------
 constexpr int kRowsLds = 132;  // floats of a row's state in LDS
 
@@ -632,19 +653,30 @@ __device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int
     const int cnt = ceil_div(je - j, kRowsWaves);
     RowsTab T;
     load_tab(a, b, kh, sq, j, je, T);
-    RowsGroup<BITS> x[2];
-    load_group<BITS>(a, kh, head_off, T, 0, x[0]);
-    for (int i = 0; i < cnt; i += 2) {
+    RowsGroup<BITS> x;
+    load_group_k<BITS>(a, kh, head_off, T, 0, x);
+    load_group_v<BITS>(a, kh, head_off, T, 0, x);
+    // each half's next codes are requested as soon as its registers are free
+    for (int i = 0; i < cnt; ++i) {
+      const int at = i & 63;
+      const bool live = __builtin_amdgcn_readlane(T.slot, at) >= 0;
+      const float sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sk), at));
+      const float sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sv), at));
+      if (at == 63) load_tab(a, b, kh, sq, j + kRowsWaves * (i + 1), je, T);
+      f4 S[NT][4];
+      group_scores<BITS, NT>(x, Q, S, szk);
+      load_group_k<BITS>(a, kh, head_off, T, (i + 1) & 63, x);
+      if (live) {
+        constexpr float up = 1 << kDown<BITS>;
+        float ex, inv;
+        value_scale(sv, up, ex, inv);
+        u32x4_t P[NT][2];
 #pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int at = (i + p) & 63;
-        const bool live = __builtin_amdgcn_readlane(T.slot, at) >= 0;
-        const float sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sk), at));
-        const float sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sv), at));
-        if (at == 63) load_tab(a, b, kh, sq, j + kRowsWaves * (i + p + 1), je, T);
-        load_group<BITS>(a, kh, head_off, T, (i + p + 1) & 63, x[1 - p]);
-        if (live && i + p < cnt) step_group<BITS, NT>(a, x[p], sk, sv, Q, st, szk);
+        for (int t = 0; t < NT; ++t)
+          rows_softmax<NT, BITS == 4, false>(st, t, S[t], sk * (a.sm_log2e * up), ex, inv, 0, P[t]);
+        group_values<BITS, NT>(x, P, st);
       }
+      load_group_v<BITS>(a, kh, head_off, T, (i + 1) & 63, x);
     }
     j += kRowsWaves * cnt;
   }
@@ -662,15 +694,18 @@ __device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int
 
 template <int NT>
 __global__ __launch_bounds__(64 * kRowsWaves) void k_attn_rows(RowsArgs a) {
-  __shared__ __attribute__((aligned(16))) float part[kRowsWaves][16 * NT][kRowsLds];
+  __shared__ __attribute__((aligned(16))) float part[kRowsWaves][16][kRowsLds];
   __shared__ uint2 szk[kRowsWaves][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g4 = lane >> 4;
-  int u = blockIdx.x;
-  const int rt = u % a.ntiles_row;
-  u /= a.ntiles_row;
+  // work-groups go to the eight XCDs in turn: the row tiles of a chunk, which read the
+  // same codes, to one of them
+  const unsigned span = 8u * a.ntiles_row;
+  const int rt = (int)(blockIdx.x % span >> 3);
+  int u = (int)(blockIdx.x / span * 8 + (blockIdx.x & 7));
   const int s = u % a.nchunk;
   u /= a.nchunk;
   const int b = u / a.Hkv, kh = u - b * a.Hkv;
+  if (b >= a.B) return;
   const RowsSeq sq = rows_seq(a, b);
   const int base = 16 * NT * rt, rows = a.G * sq.tl;
   if (base >= rows || s >= max(sq.nparts, 1)) return;
@@ -693,11 +728,13 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_attn_rows(RowsArgs a) {
     rows_tiles<2, NT>(a, b, kh, head_off, sq, j0, j1, Q, st, szk[w]);
   else
     rows_tiles<4, NT>(a, b, kh, head_off, sq, j0, j1, Q, st, szk[w]);
-  // the waves' states to LDS, and their merge
+  // the waves' states to LDS, and their merge: 16 lanes a row
+  const int row = threadIdx.x >> 4, c0 = 8 * (threadIdx.x & 15);
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const float l = add_xor32(st.l[t] + __shfl_xor(st.l[t], 16));
-    float* p = part[w][16 * t + n];
+    float* p = part[w][n];
+    if (t > 0) __syncthreads();
     if (g4 == 0) *reinterpret_cast<float2*>(p) = make_float2(st.m[t], l);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -705,59 +742,78 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_attn_rows(RowsArgs a) {
       *reinterpret_cast<f4*>(d) = f4{st.o[t][0][r], st.o[t][1][r], st.o[t][2][r], st.o[t][3][r]};
       *reinterpret_cast<f4*>(d + 4) = f4{st.o[t][4][r], st.o[t][5][r], st.o[t][6][r], st.o[t][7][r]};
     }
-  }
-  __syncthreads();
-  const int c0 = 8 * (threadIdx.x & 15);
-  for (int row = threadIdx.x >> 4; row < 16 * NT; row += 4 * kRowsWaves) {
-    if (base + row >= rows) break;
+    __syncthreads();
+    const int at_row = base + 16 * t + row;
+    if (at_row >= rows) continue;
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kRowsWaves; ++i) m = fmaxf(m, part[i][row][0]);
-    float l = 0.0f, o[8] = {};
+    float ls = 0.0f, o[8] = {};
 #pragma unroll
     for (int i = 0; i < kRowsWaves; ++i) {
-      const float* p = part[i][row];
-      const float f = p[0] == m ? 1.0f : __builtin_amdgcn_exp2f(p[0] - m);
-      l = __builtin_fmaf(f, p[1], l);
+      const float* q = part[i][row];
+      const float f = q[0] == m ? 1.0f : __builtin_amdgcn_exp2f(q[0] - m);
+      ls = __builtin_fmaf(f, q[1], ls);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(f, p[4 + c0 + e], o[e]);
+      for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(f, q[4 + c0 + e], o[e]);
     }
-    const int h = (base + row) / sq.tl;
-    const long at = ((long)b * a.Hq + kh * a.G + h) * a.T + (base + row - h * sq.tl);
+    const int h = at_row / sq.tl;
+    const long at = ((long)b * a.Hq + kh * a.G + h) * a.T + (at_row - h * sq.tl);
     if (sq.nparts <= 1) {
-      rows_store(a, at, c0, m, l, o);
+      rows_store(a, at, c0, m, ls, o);
     } else {
-      float* p = a.ws + (at * a.nchunk + s) * kWsStride;
-      *reinterpret_cast<float4*>(p + kWsO + c0) = make_float4(o[0], o[1], o[2], o[3]);
-      *reinterpret_cast<float4*>(p + kWsO + c0 + 4) = make_float4(o[4], o[5], o[6], o[7]);
-      if (c0 == 0) *reinterpret_cast<float2*>(p) = make_float2(m, l);
+      float* q = a.ws + (at * a.nchunk + s) * kWsStride;
+      *reinterpret_cast<float4*>(q + kWsO + c0) = make_float4(o[0], o[1], o[2], o[3]);
+      *reinterpret_cast<float4*>(q + kWsO + c0 + 4) = make_float4(o[4], o[5], o[6], o[7]);
+      if (c0 == 0) *reinterpret_cast<float2*>(q) = make_float2(m, ls);
     }
   }
 }
 
-// Rows of several chunks: 16 lanes merge a row's states, in the order of the chunks.
+// Rows of several chunks: a wave merges a row's states, a quarter of them in each 16
+// lanes (four at a time, their loads together), then the quarters.
 __global__ __launch_bounds__(256) void k_rows_merge(RowsArgs a) {
-  const long at = (long)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const long at = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (at >= (long)a.B * a.Hq * a.T) return;
-  const int c0 = 8 * (threadIdx.x & 15);
+  const int lane = threadIdx.x & 63, c0 = 8 * (lane & 15);
   const long bh = at / a.T;
   const int b = (int)(bh / a.Hq);
   const RowsSeq sq = rows_seq(a, b);
   if (at - bh * a.T >= sq.tl || sq.nparts <= 1) return;
-  const float* p = a.ws + at * a.nchunk * kWsStride;
-  float m = -INFINITY;
-  for (int i = 0; i < sq.nparts; ++i) m = fmaxf(m, p[(long)i * kWsStride]);
-  float l = 0.0f, o[8] = {};
-  for (int i = 0; i < sq.nparts; ++i, p += kWsStride) {
-    const float f = p[0] == m ? 1.0f : __builtin_amdgcn_exp2f(p[0] - m);
-    l = __builtin_fmaf(f, p[1], l);
-    const float4 x = *reinterpret_cast<const float4*>(p + kWsO + c0);
-    const float4 y = *reinterpret_cast<const float4*>(p + kWsO + c0 + 4);
-    const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+  const float* ws = a.ws + at * a.nchunk * kWsStride;
+  float m = -INFINITY, l = 0.0f, o[8] = {};
+  for (int i0 = lane >> 4; i0 < sq.nparts; i0 += 16) {
+    float pm[4], pl[4];
+    float4 x[4], y[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(f, v[e], o[e]);
+    for (int k = 0; k < 4; ++k) {
+      const int i = i0 + 4 * k;
+      pm[k] = -INFINITY;
+      pl[k] = 0.0f;
+      x[k] = y[k] = make_float4(0, 0, 0, 0);
+      if (i < sq.nparts) {
+        const float* p = ws + (long)i * kWsStride;
+        pm[k] = p[0];
+        pl[k] = p[1];
+        x[k] = *reinterpret_cast<const float4*>(p + kWsO + c0);
+        y[k] = *reinterpret_cast<const float4*>(p + kWsO + c0 + 4);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float v[8] = {x[k].x, x[k].y, x[k].z, x[k].w, y[k].x, y[k].y, y[k].z, y[k].w};
+      rows_join(m, l, o, pm[k], pl[k], v);
+    }
   }
-  rows_store(a, at, c0, m, l, o);
+#pragma unroll
+  for (int d = 16; d <= 32; d += d) {
+    float v[8];
+    const float pm = __shfl_xor(m, d), pl = __shfl_xor(l, d);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __shfl_xor(o[e], d);
+    rows_join(m, l, o, pm, pl, v);
+  }
+  if (lane < 16) rows_store(a, at, c0, m, l, o);
 }
 
 // Tiles of 16 query rows that a wave takes: a second one shares the codes' expansion.
@@ -773,15 +829,19 @@ inline int rows_chunks(int B, int Hkv, int G, int T, int max_tiles) {
   return (int)(want < most ? (want > 1 ? want : 1) : (most > 1 ? most : 1));
 }
 
+inline long rows_groups(const RowsArgs& a) {
+  return ((long)a.B * a.Hkv * a.nchunk + 7) / 8 * 8 * a.ntiles_row;
+}
+
 inline hipError_t launch_attn_rows(const RowsArgs& a, hipStream_t stream) {
-  const long groups = (long)a.B * a.Hkv * a.ntiles_row * a.nchunk;
+  const dim3 groups((unsigned)rows_groups(a)), threads(64 * kRowsWaves);
   if (rows_nt(a.G, a.T) == 1)
-    hipLaunchKernelGGL((k_attn_rows<1>), dim3((unsigned)groups), dim3(64 * kRowsWaves), 0, stream, a);
+    hipLaunchKernelGGL((k_attn_rows<1>), groups, threads, 0, stream, a);
   else
-    hipLaunchKernelGGL((k_attn_rows<2>), dim3((unsigned)groups), dim3(64 * kRowsWaves), 0, stream, a);
+    hipLaunchKernelGGL((k_attn_rows<2>), groups, threads, 0, stream, a);
   if (a.nchunk > 1) {
     const long rows = (long)a.B * a.Hq * a.T;
-    hipLaunchKernelGGL(k_rows_merge, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL(k_rows_merge, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a);
   }
   return hipGetLastError();
 }

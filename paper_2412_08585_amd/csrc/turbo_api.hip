@@ -695,11 +695,14 @@ static int attn_rows_impl(turbo::RowsArgs& a, const turbo_kv_cache* cache,
   st = check_tail(tail, B, Hkv);
   if (st != TURBO_OK) return st;
   if (tiles > 0x7fffffffL || (long)B * Hq * T > 0x7fffffffL) return TURBO_ERR_INVALID_ARG;
+  a.B = B;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
   a.T = T;
   a.G = Hq / Hkv;
   a.ntiles_row = turbo::rows_tiles_per_head(a.G, T);
   a.nchunk = turbo::rows_chunks(B, Hkv, a.G, T, (int)tiles);
-  if ((long)B * Hkv * a.ntiles_row * a.nchunk > 0x7fffffffL) return TURBO_ERR_INVALID_ARG;
+  if (turbo::rows_groups(a) > 0x7fffffffL) return TURBO_ERR_INVALID_ARG;
   const size_t need = rows_workspace(B, Hq, Hkv, T, tiles);
   if (need > 0 && (!workspace || workspace_bytes < need)) return TURBO_ERR_WORKSPACE_TOO_SMALL;
   st = check_device();
@@ -713,9 +716,6 @@ static int attn_rows_impl(turbo::RowsArgs& a, const turbo_kv_cache* cache,
   a.block_table = block_table;
   a.group_table = group_table;
   a.max_groups = max_groups_per_seq;
-  a.B = B;
-  a.Hq = Hq;
-  a.Hkv = Hkv;
   a.sm_log2e = (float)(sm_scale * 1.4426950408889634);
   if (tail) {
     a.tk = tail->k;
