@@ -524,63 +524,68 @@ def turbo_attn_prefill_q8(q8: torch.Tensor, s_q: torch.Tensor, k8, v8, s_k, s_v,
 
 # ---- sparse and speculative decoding -------------------------------------------
 # These calls check every tensor (type, shape, device, contiguity) and run on the
-# tensors' device, whichever is current.
+# tensors' device, whichever is current.  A device is compared by its index (-1: the
+# CPU), which torch returns in a fraction of the time of a device object.
 
 
-def _arg(t: torch.Tensor, name: str, dtype, shape, device) -> int:
-    """Address of t, which must have this type and shape and lie on device."""
-    if t.dtype != dtype or t.shape != shape or t.device != device:
-        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on {device}, but is {t.dtype} "
+def _arg(t: torch.Tensor, name: str, dtype, shape, index: int) -> int:
+    """Address of t, which must be contiguous with this type and shape on device index."""
+    if (t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous()):
+        return t.data_ptr()
+    if t.dtype != dtype or t.shape != shape or t.get_device() != index:
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)} on device {index}, but is {t.dtype} "
                          f"{tuple(t.shape)} on {t.device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _shape(t: torch.Tensor, name: str, dims: int):
-    if t.dim() != dims:
-        raise ValueError(f"{name} must have {dims} dimensions, but is {tuple(t.shape)}")
-    return t.shape
+    s = t.shape
+    if len(s) != dims:
+        raise ValueError(f"{name} must have {dims} dimensions, but is {tuple(s)}")
+    return s
 
 
 def _cache_args(cache: PagedKVCache, tail: Optional[KVTail], B: int, seq_lens: torch.Tensor,
-                block_table: torch.Tensor, group_table: torch.Tensor, device):
+                block_table: torch.Tensor, group_table: torch.Tensor, index: int):
     """(cache struct, tail struct, lengths, block table, group table, max_groups)."""
     mg = _shape(group_table, "group_table", 2)[1]
     for t in (cache.pages, cache.group_meta, cache.group_scale):
-        if t.device != device or not t.is_contiguous():
-            raise ValueError(f"the cache must be contiguous on {device}")
+        if t.get_device() != index or not t.is_contiguous():
+            raise ValueError(f"the cache must be contiguous on device {index}")
     ts = None
     if tail is not None:
         for t in (tail.k, tail.v, tail.scale):
-            if t.device != device or not t.is_contiguous():
-                raise ValueError(f"the buffer must be contiguous on {device}")
+            if t.get_device() != index or not t.is_contiguous():
+                raise ValueError(f"the buffer must be contiguous on device {index}")
         ts = tail._packed()
     i32 = torch.int32
-    return (cache._packed(), ts, _arg(seq_lens, "seq_lens", i32, (B,), device),
-            _arg(block_table, "block_table", i32, (B, 4 * mg), device),
-            _arg(group_table, "group_table", i32, (B, mg), device), mg)
+    return (cache._packed(), ts, _arg(seq_lens, "seq_lens", i32, (B,), index),
+            _arg(block_table, "block_table", i32, (B, 4 * mg), index),
+            _arg(group_table, "group_table", i32, (B, mg), index), mg)
 
 
-def _scratch(workspace: Optional[torch.Tensor], device):
+def _scratch(workspace: Optional[torch.Tensor], index: int):
     """(address, bytes) of a workspace."""
     if workspace is None:
         return None, 0
-    if workspace.device != device or not workspace.is_contiguous():
-        raise ValueError(f"workspace must be contiguous on {device}")
+    if workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous on device {index}")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
-def _launch(device, what: str, *args):
+def _launch(index: int, what: str, *args):
     """The library's `what` with args and the device's current stream, on that device."""
-    stream = _stream(device)
+    if index < 0:
+        raise ValueError("Expected tensors on a cuda device")
     fn = getattr(lib(), what)
-    if device.index == torch.cuda.current_device():
+    stream = torch._C._cuda_getCurrentRawStream(index)
+    if index == torch.cuda.current_device():
         status = fn(*args, stream)
     else:
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             status = fn(*args, stream)
-    _check(status, what)
+    if status != 0:
+        _check(status, what)
 
 
 def _words(nbytes: int, device) -> Optional[torch.Tensor]:
@@ -612,15 +617,15 @@ def turbo_select_groups(q: torch.Tensor, cache: PagedKVCache, seq_lens: torch.Te
     last keep_last always).  Returns int32 [B][Hkv][num_select], ascending, -1
     behind the last."""
     B, Hq, d = _shape(q, "q", 3)
-    dev, Hkv = q.device, cache.num_kv_heads
+    dev, Hkv = q.get_device(), cache.num_kv_heads
     qp = _arg(q, "q", torch.float16, (B, Hq, HEAD_DIM), dev)
     cs, _, sl, bt, gt, mg = _cache_args(cache, None, B, seq_lens, block_table, group_table, dev)
     if num_select < 1:
         raise ValueError("num_select must be at least 1")
-    sel = torch.empty(B, Hkv, num_select, dtype=torch.int32, device=dev) if out is None else out
+    sel = torch.empty(B, Hkv, num_select, dtype=torch.int32, device=q.device) if out is None else out
     sp = _arg(sel, "out", torch.int32, (B, Hkv, num_select), dev)
     if workspace is None:
-        workspace = select_workspace(B, Hq, mg, dev)
+        workspace = select_workspace(B, Hq, mg, q.device)
     wp, wbytes = _scratch(workspace, dev)
     _launch(dev, "turbo_select_groups", qp, cs, sl, bt, gt, mg, B, Hq, int(num_select),
             int(keep_first), int(keep_last), wp, wbytes, sp)
@@ -636,7 +641,7 @@ def turbo_attn_selected(q: torch.Tensor, cache: PagedKVCache, seq_lens: torch.Te
     [B][Hkv][num_select] of the cache (and the buffer when tail is given), with
     the exponential itself.  Returns o (and lse)."""
     B, Hq, d = _shape(q, "q", 3)
-    dev, Hkv = q.device, cache.num_kv_heads
+    dev, Hkv = q.get_device(), cache.num_kv_heads
     qp = _arg(q, "q", torch.float16, (B, Hq, HEAD_DIM), dev)
     cs, ts, sl, bt, gt, mg = _cache_args(cache, tail, B, seq_lens, block_table, group_table, dev)
     k = _shape(selected, "selected", 3)[2]
@@ -645,10 +650,10 @@ def turbo_attn_selected(q: torch.Tensor, cache: PagedKVCache, seq_lens: torch.Te
     op = _arg(o, "out", torch.float16, q.shape, dev)
     lse = lse_out
     if lse is None and return_lse:
-        lse = torch.empty(B, Hq, dtype=torch.float32, device=dev)
+        lse = torch.empty(B, Hq, dtype=torch.float32, device=q.device)
     lp = None if lse is None else _arg(lse, "lse_out", torch.float32, (B, Hq), dev)
     if workspace is None:
-        workspace = selected_workspace(B, Hq, Hkv, k, dev, tail is not None)
+        workspace = selected_workspace(B, Hq, Hkv, k, q.device, tail is not None)
     wp, wbytes = _scratch(workspace, dev)
     _launch(dev, "turbo_attn_selected", qp, cs, ts, sl, bt, gt, mg, sp, k, B, Hq,
             _scale(HEAD_DIM, sm_scale), wp, wbytes, op, lp)
@@ -660,12 +665,12 @@ def turbo_tree_mask(parents: torch.Tensor, tree_lens: torch.Tensor, out=None, de
     trees, from parents int32 [B][T] (an earlier node, or -1) and tree_lens int32
     [B]."""
     B, T = _shape(parents, "parents", 2)
-    dev = parents.device
+    dev = parents.get_device()
     pp = _arg(parents, "parents", torch.int32, (B, T), dev)
     lp = _arg(tree_lens, "tree_lens", torch.int32, (B,), dev)
     W = (T + 63) // 64
-    mask = torch.empty(B, T, W, dtype=torch.int64, device=dev) if out is None else out
-    depth = torch.empty(B, T, dtype=torch.int32, device=dev) if depth_out is None else depth_out
+    mask = torch.empty(B, T, W, dtype=torch.int64, device=parents.device) if out is None else out
+    depth = torch.empty(B, T, dtype=torch.int32, device=parents.device) if depth_out is None else depth_out
     _launch(dev, "turbo_tree_mask", pp, lp, B, T, _arg(mask, "out", torch.int64, (B, T, W), dev),
             _arg(depth, "depth_out", torch.int32, (B, T), dev))
     return mask, depth
@@ -683,7 +688,7 @@ def turbo_attn_tree(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor,
     up to the row's own), with the exponential itself.  Rows of nodes from
     tree_lens[b] on are not written.  Returns o (and lse)."""
     B, Hq, T, d = _shape(q, "q", 4)
-    dev, Hkv, f16 = q.device, cache.num_kv_heads, torch.float16
+    dev, Hkv, f16 = q.get_device(), cache.num_kv_heads, torch.float16
     qp = _arg(q, "q", f16, (B, Hq, T, HEAD_DIM), dev)
     kp = _arg(k_tree, "k_tree", f16, (B, Hkv, T, HEAD_DIM), dev)
     vp = _arg(v_tree, "v_tree", f16, (B, Hkv, T, HEAD_DIM), dev)
@@ -696,10 +701,10 @@ def turbo_attn_tree(q: torch.Tensor, k_tree: torch.Tensor, v_tree: torch.Tensor,
     op = _arg(o, "out", f16, q.shape, dev)
     lse = lse_out
     if lse is None and return_lse:
-        lse = torch.empty(B, Hq, T, dtype=torch.float32, device=dev)
+        lse = torch.empty(B, Hq, T, dtype=torch.float32, device=q.device)
     lp = None if lse is None else _arg(lse, "lse_out", torch.float32, (B, Hq, T), dev)
     if workspace is None:
-        workspace = tree_workspace(B, Hq, Hkv, T, mg, dev, tail is not None)
+        workspace = tree_workspace(B, Hq, Hkv, T, mg, q.device, tail is not None)
     wp, wbytes = _scratch(workspace, dev)
     _launch(dev, "turbo_attn_tree", qp, kp, vp, mp, tp, cs, ts, sl, bt, gt, mg, B, Hq, T,
             _scale(HEAD_DIM, sm_scale), wp, wbytes, op, lp)
@@ -713,7 +718,7 @@ def turbo_append_path(k_tree: torch.Tensor, v_tree: torch.Tensor, path: torch.Te
     them) of k_tree, v_tree fp16 [B][Hkv][T][128] at positions seq_lens onwards, as
     one turbo_append_kv each would."""
     B, Hkv, T, d = _shape(k_tree, "k_tree", 4)
-    dev = k_tree.device
+    dev = k_tree.get_device()
     kp = _arg(k_tree, "k_tree", torch.float16, (B, Hkv, T, HEAD_DIM), dev)
     vp = _arg(v_tree, "v_tree", torch.float16, (B, Hkv, T, HEAD_DIM), dev)
     P = _shape(path, "path", 2)[1]

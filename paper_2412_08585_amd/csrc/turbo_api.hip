@@ -634,7 +634,7 @@ int turbo_select_groups(const void* q, const turbo_kv_cache* cache, const int32_
   int page_bytes = 0;
   int st = check_cache(cache, Hkv, &a.int2_mask, &page_bytes);
   if (st != TURBO_OK) return st;
-  if ((long)B * Hkv * turbo::ceil_div(max_groups_per_seq, turbo::kBoundGroups) > 0x7fffffffL)
+  if ((long)B * Hkv * turbo::ceil_div(max_groups_per_seq, 64) > 0x7fffffffL)
     return TURBO_ERR_INVALID_ARG;
   if (!workspace || workspace_bytes < turbo_select_workspace_bytes(B, Hq, max_groups_per_seq))
     return TURBO_ERR_WORKSPACE_TOO_SMALL;
