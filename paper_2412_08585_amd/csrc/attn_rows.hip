@@ -65,6 +65,7 @@ struct RowsArgs {
   const float* tscale;
   int ntiles_row;            // row tiles in the grid
   int nchunk;                // chunks in the grid
+  int min_len;               // tiles of a chunk, at least
   float* ws;                 // [B][Hq][T][nchunk][132]: m, l, -, -, O[128]
   unsigned short* o;         // fp16 [B][Hq][T][128]
   float* lse;                // [B][Hq][T] or null
@@ -92,7 +93,7 @@ __device__ __forceinline__ RowsSeq rows_seq(const RowsArgs& a, int b) {
   s.tl = a.tree_lens ? min(max(a.tree_lens[b], 0), a.T) : a.T;
   s.nlist = a.sel ? a.nsel : s.ng;
   s.ntile = s.nlist + (s.nt > 0) + (a.kt ? (s.tl + 63) / 64 : 0);
-  s.len = max(kRowsWaves, ceil_div(s.ntile, a.nchunk));
+  s.len = max(a.min_len, ceil_div(s.ntile, a.nchunk));
   s.nparts = ceil_div(s.ntile, s.len);
   return s;
 }
@@ -290,10 +291,11 @@ struct RowsTab {
   float sk, sv;
 };
 
-// Lane i: the tile j + i * kRowsWaves of the list, attended below j1.
+// Lane i: the tile j + i * STEP of the list, attended below j1.
+template <int STEP>
 __device__ __forceinline__ void load_tab(const RowsArgs& a, int b, int kh, const RowsSeq& sq, int j,
                                          int j1, RowsTab& T) {
-  j += (int)(threadIdx.x & 63) * kRowsWaves;
+  j += (int)(threadIdx.x & 63) * STEP;
   bool ok = j < j1;
   int g = ok ? j : 0;
   if (a.sel) g = ok ? a.sel[((long)b * a.Hkv + kh) * a.nsel + j] : 0;
@@ -507,6 +509,59 @@ __device__ __forceinline__ bool nonfinite_h2(unsigned x) {
   return (x & 0x7c00u) == 0x7c00u || (x & 0x7c000000u) == 0x7c000000u;
 }
 
+// Which of the lane's 16 nodes of tile j a row (node `node` of the tree) sees.
+__device__ __forceinline__ unsigned nodes_visible(const RowsArgs& a, int b, int j, int tl, long at,
+                                                  int node) {
+  const int g4 = (threadIdx.x & 63) >> 4;
+  const int live = min(max(tl - 64 * j - 16 * g4, 0), 16);
+  unsigned long long w = 0;
+  if (at >= 0) {
+    if (a.mask) {
+      w = a.mask[((long)b * a.T + node) * a.mwords + j];
+    } else {
+      const int c = node + 1 - 64 * j;  // nodes of this tile up to the row's own
+      w = c >= 64 ? ~0ull : (c > 0 ? (1ull << c) - 1ull : 0ull);
+    }
+  }
+  return (unsigned)(w >> (16 * g4)) & ((1u << live) - 1u);
+}
+
+// Adds the values of tile j (rows of vb) that are not finite to the rows that see
+// their node.
+template <int NT, bool PAIR4>
+__device__ void nodes_nonfinite(const RowsArgs& a, const unsigned short* vb, int j, int tl,
+                                const u32x4_t (&P)[NT][2], const unsigned (&vis)[NT],
+                                RowsState<NT>& st) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
+  const int cnt = min(tl - 64 * j, 64);
+  for (int i = 0; i < cnt; ++i) {
+    const unsigned short* vr = vb + (64L * j + i) * 128 + 32 * g4;
+    const int from = 16 * (i >> 4) + n;  // lane that holds the row's p of token i
+    // register (ks, jj) and half of token i & 15 of the page
+    const int tok = i & 15;
+    const int reg = PAIR4 ? (tok >> 3) * 4 + (tok & 3) : tok & 7;
+    const bool high = PAIR4 ? tok & 4 : tok & 8;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      unsigned w = 0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w = reg == k ? P[t][k >> 2][k & 3] : w;
+      if (high) w >>= 16;
+      const unsigned pw = __shfl((int)(w & 0xffffu), from);
+      const unsigned seen = __shfl((int)vis[t], from) >> tok;
+      const float p = (float)__builtin_bit_cast(_Float16, (unsigned short)pw);
+      if (!(seen & 1u)) continue;
+#pragma unroll
+      for (int cb = 0; cb < 8; ++cb)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const unsigned short x = vr[8 * r + cb];
+          if ((x & 0x7c00u) == 0x7c00u) st.o[t][cb][r] += p * (float)__builtin_bit_cast(_Float16, x);
+        }
+    }
+  }
+}
+
 // Nodes 64 j .. of the sequence's tl; Q in order kOrdNat.  A value that is not
 // finite must not reach the rows that do not see its node (0 * NaN): it takes no
 // part in the products and is added to the rows that do afterwards.
@@ -531,21 +586,11 @@ __device__ __forceinline__ void step_nodes(const RowsArgs& a, int b, long u, int
         S[t][mb] = mfma_h(u32x4_t{A.x, A.y, A.z, A.w}, Q.x[t][ks], S[t][mb]);
     }
   }
-  const int live = min(max(tl - 64 * j - 16 * g4, 0), 16);
   u32x4_t P[NT][2];
   unsigned vis[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    unsigned long long w = 0;
-    if (Q.at[t] >= 0) {
-      if (a.mask) {
-        w = a.mask[((long)b * a.T + Q.node[t]) * a.mwords + j];
-      } else {
-        const int c = Q.node[t] + 1 - 64 * j;  // nodes of this tile up to the row's own
-        w = c >= 64 ? ~0ull : (c > 0 ? (1ull << c) - 1ull : 0ull);
-      }
-    }
-    vis[t] = (unsigned)(w >> (16 * g4)) & ((1u << live) - 1u);
+    vis[t] = nodes_visible(a, b, j, tl, Q.at[t], Q.node[t]);
     rows_softmax<NT, true, true>(st, t, S[t], a.sm_log2e, 0.0f, 1.0f, vis[t], P[t]);
   }
   bool bad = false;
@@ -583,33 +628,7 @@ __device__ __forceinline__ void step_nodes(const RowsArgs& a, int b, long u, int
       for (int t = 0; t < NT; ++t) st.o[t][cb] = mfma_h(A, P[t][ks], st.o[t][cb]);
     }
   }
-  if (__any(bad)) {
-    const int cnt = min(tl - 64 * j, 64);
-    for (int i = 0; i < cnt; ++i) {
-      const unsigned short* vr = vb + (64L * j + i) * 128 + 32 * g4;
-      const int from = 16 * (i >> 4) + n;  // lane that holds the row's p of token i
-      const int reg = i & 15;              // P[t][ks][jj]: ks = reg >> 3, jj = reg & 3
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        unsigned w = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          w = ((reg >> 3) * 4 + (reg & 3)) == k ? P[t][k >> 2][k & 3] : w;
-        if (reg & 4) w >>= 16;
-        const unsigned pw = __shfl((int)(w & 0xffffu), from);
-        const unsigned seen = __shfl((int)vis[t], from) >> (i & 15);
-        const float p = (float)__builtin_bit_cast(_Float16, (unsigned short)pw);
-        if (!(seen & 1u)) continue;
-#pragma unroll
-        for (int cb = 0; cb < 8; ++cb)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const unsigned short x = vr[8 * r + cb];
-            if ((x & 0x7c00u) == 0x7c00u) st.o[t][cb][r] += p * (float)__builtin_bit_cast(_Float16, x);
-          }
-      }
-    }
-  }
+  if (__any(bad)) nodes_nonfinite<NT, true>(a, vb, j, tl, P, vis, st);
 }
 
 // Row `at` of o and lse from its merged state (8 channels from c0).
@@ -652,7 +671,7 @@ __device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int
     load_q<NT, BITS == 4 ? kOrd4 : kOrd2>(a, Q);
     const int cnt = ceil_div(je - j, kRowsWaves);
     RowsTab T;
-    load_tab(a, b, kh, sq, j, je, T);
+    load_tab<kRowsWaves>(a, b, kh, sq, j, je, T);
     RowsGroup<BITS> x;
     load_group_k<BITS>(a, kh, head_off, T, 0, x);
     load_group_v<BITS>(a, kh, head_off, T, 0, x);
@@ -662,7 +681,7 @@ __device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int
       const bool live = __builtin_amdgcn_readlane(T.slot, at) >= 0;
       const float sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sk), at));
       const float sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sv), at));
-      if (at == 63) load_tab(a, b, kh, sq, j + kRowsWaves * (i + 1), je, T);
+      if (at == 63) load_tab<kRowsWaves>(a, b, kh, sq, j + kRowsWaves * (i + 1), je, T);
       f4 S[NT][4];
       group_scores<BITS, NT>(x, Q, S, szk);
       load_group_k<BITS>(a, kh, head_off, T, (i + 1) & 63, x);
@@ -770,6 +789,356 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_attn_rows(RowsArgs a) {
   }
 }
 
+// ---- many rows: tiles expanded once per work-group -------------------------------
+// With T * G rows per KV head the expansion of the codes, 5/6 of a tile's vector
+// instructions for 16 rows, is shared: the four waves of a work-group take 32 rows
+// each, expand a quarter of the next tile into LDS, in the order in which its lanes
+// hold the operands, and read all of this one.  Two buffers, one barrier a tile.
+constexpr int kWideRows = 128;
+
+struct WideTile {
+  u32x4_t k[4][4][64];  // [ks][mb][lane]
+  u32x4_t v[8][2][64];  // [cb][ks][lane]
+};
+
+template <int BITS>
+struct WideRaw {
+  unsigned k[BITS];     // codes of token (m, mb = wave)
+  unsigned v[BITS];     // codes of channels 8 n + 2 wave, + 1, the lane's page
+  uint2 ks, kz;
+  unsigned vs, vz;      // s^int, z^int of the two channels, low bytes
+};
+
+template <int BITS>
+__device__ __forceinline__ void wide_load(const RowsArgs& a, int kh, int head_off, const RowsTab& T,
+                                          int i, WideRaw<BITS>& x) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g4 = lane >> 4;
+  const uint8_t* kp = a.pages + tab_page(a, T, i, n >> 2) + head_off +
+                      (4 * w + (n & 3)) * 16 * BITS + 4 * BITS * g4;
+  const uint8_t* vp =
+      a.pages + tab_page(a, T, i, g4) + head_off + 256 * BITS + n * 16 * BITS + 4 * BITS * w;
+  if constexpr (BITS == 4) {
+    const uint4 c = *reinterpret_cast<const uint4*>(kp), d = *reinterpret_cast<const uint4*>(vp);
+    x.k[0] = c.x; x.k[1] = c.y; x.k[2] = c.z; x.k[3] = c.w;
+    x.v[0] = d.x; x.v[1] = d.y; x.v[2] = d.z; x.v[3] = d.w;
+  } else {
+    const uint2 c = *reinterpret_cast<const uint2*>(kp), d = *reinterpret_cast<const uint2*>(vp);
+    x.k[0] = c.x; x.k[1] = c.y;
+    x.v[0] = d.x; x.v[1] = d.y;
+  }
+  constexpr int ORD = BITS == 4 ? kOrd4 : kOrd2;
+  const int8_t* meta = tab_meta(a, T, i, kh);
+  const int8_t* mk = meta + 32 * g4 + (chan_lo<ORD>(n >> 2, n & 3) & ~3);
+  x.ks = make_uint2(*reinterpret_cast<const unsigned*>(mk),
+                    *reinterpret_cast<const unsigned*>(mk + kChanDist<ORD>));
+  x.kz = make_uint2(*reinterpret_cast<const unsigned*>(mk + 128),
+                    *reinterpret_cast<const unsigned*>(mk + 128 + kChanDist<ORD>));
+  x.vs = *reinterpret_cast<const unsigned short*>(meta + 256 + 8 * n + 2 * w);
+  x.vz = *reinterpret_cast<const unsigned short*>(meta + 384 + 8 * n + 2 * w);
+}
+
+template <int BITS>
+__device__ __forceinline__ void wide_expand(const WideRaw<BITS>& x, WideTile& d, uint2* szk) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g4 = lane >> 4;
+  {
+    const int sh = 8 * (n & 3);
+    const unsigned s = scale_h2(((x.ks.x >> sh) & 0xffu) | (((x.ks.y >> sh) & 0xffu) << 16));
+    const unsigned z = zero_h2(((x.kz.x >> sh) & 0xffu) | (((x.kz.y >> sh) & 0xffu) << 16));
+    wave_sync();
+    szk[lane] = make_uint2(n & 1 ? scale_at<BITS>(s, 1) : scale_at<BITS>(s, 0), zero_at<BITS>(z));
+    wave_sync();
+  }
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) {
+    u32x4_t A;
+#pragma unroll
+    for (int jj = 0; jj < 4; ++jj) {
+      const uint2 sz = szk[16 * g4 + 4 * ks + jj];
+      const unsigned c = BITS == 4 ? code_pair<BITS>(x.k[ks], jj)
+                                   : code_pair<BITS>(x.k[ks >> 1], 4 * (ks & 1) + jj);
+      A[jj] = h2_fma(c, sz.x, sz.y);
+    }
+    d.k[ks][w][lane] = A;
+  }
+  const unsigned s = scale_h2(__builtin_amdgcn_perm(0u, x.vs, 0x0c010c00u));
+  const unsigned z = zero_h2(__builtin_amdgcn_perm(0u, x.vz, 0x0c010c00u));
+  const unsigned s0 = scale_at<BITS>(s, 0), s1 = scale_at<BITS>(s, 1), zd = zero_at<BITS>(z);
+#pragma unroll
+  for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      u32x4_t A;
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj) {
+        const unsigned c = BITS == 4 ? code_pair<BITS>(x.v[2 * hi + ks], jj)
+                                     : code_pair<BITS>(x.v[hi], 4 * ks + jj);
+        A[jj] = h2_fma(c, h2_splat(jj & 1 ? s1 : s0, hi), h2_splat(zd, hi));
+      }
+      d.v[2 * w + hi][ks][lane] = A;
+    }
+}
+
+// The buffer's 64 rows (those past the last are masked), as the codes of the head's
+// groups are ordered.
+template <int BITS>
+__device__ __forceinline__ void wide_buffer(const RowsArgs& a, long u, WideTile& d) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g4 = lane >> 4;
+  constexpr int ORD = BITS == 4 ? kOrd4 : kOrd2;
+  const int8_t* kr = a.tk + (u * 64 + 16 * (n >> 2) + 4 * w + (n & 3)) * 128 + 32 * g4;
+  unsigned kw[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) kw[i] = reinterpret_cast<const unsigned*>(kr)[i] ^ 0x80808080u;
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) {
+    u32x4_t A;
+#pragma unroll
+    for (int jj = 0; jj < 4; ++jj) {
+      const int c = chan_lo<ORD>(ks, jj), e = c + kChanDist<ORD>;
+      A[jj] = int8_pair(__builtin_amdgcn_perm(kw[e >> 2], kw[c >> 2], 0x0c040c00u + 0x00010001u * (c & 3)));
+    }
+    d.k[ks][w][lane] = A;
+  }
+#pragma unroll
+  for (int hi = 0; hi < 2; ++hi) {
+    const int8_t* vr = a.tv + (u * 128 + 8 * n + 2 * w + hi) * 64 + 16 * g4;
+    unsigned vw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vw[i] = reinterpret_cast<const unsigned*>(vr)[i] ^ 0x80808080u;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      u32x4_t A;
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj) {
+        const int lo = BITS == 4 ? 2 * ks : ks, up = BITS == 4 ? 2 * ks + 1 : ks + 2;
+        A[jj] = int8_pair(__builtin_amdgcn_perm(vw[up], vw[lo], 0x0c040c00u + 0x00010001u * jj));
+      }
+      d.v[2 * w + hi][ks][lane] = A;
+    }
+  }
+}
+
+// Nodes 64 j ..; returns whether a value was not finite (it is zero in the tile).
+template <int BITS>
+__device__ __forceinline__ bool wide_nodes(const RowsArgs& a, long u, int j, int tl, WideTile& d) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g4 = lane >> 4;
+  constexpr int ORD = BITS == 4 ? kOrd4 : kOrd2;
+  const int tok = 64 * j + 16 * (n >> 2) + 4 * w + (n & 3);
+  unsigned raw[16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    u4_any x = {0, 0, 0, 0};
+    if (tok < tl) x = reinterpret_cast<const u4_any*>(a.kt + (u * a.T + tok) * 128 + 32 * g4)[i];
+    raw[4 * i] = x.x; raw[4 * i + 1] = x.y; raw[4 * i + 2] = x.z; raw[4 * i + 3] = x.w;
+  }
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) {
+    u32x4_t A;
+#pragma unroll
+    for (int jj = 0; jj < 4; ++jj) {
+      const int c = chan_lo<ORD>(ks, jj);
+      A[jj] = __builtin_amdgcn_perm(raw[(c + kChanDist<ORD>) >> 1], raw[c >> 1],
+                                    c & 1 ? 0x07060302u : 0x05040100u);
+    }
+    d.k[ks][w][lane] = A;
+  }
+  typedef unsigned u1_any __attribute__((aligned(2)));
+  unsigned v[16];
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int t = 64 * j + 16 * g4 + i;
+    v[i] = t < tl ? *reinterpret_cast<const u1_any*>(a.vt + (u * a.T + t) * 128 + 8 * n + 2 * w) : 0u;
+    bad = bad || nonfinite_h2(v[i]);
+    if ((v[i] & 0x7c00u) == 0x7c00u) v[i] &= 0xffff0000u;
+    if ((v[i] & 0x7c000000u) == 0x7c000000u) v[i] &= 0xffffu;
+  }
+#pragma unroll
+  for (int hi = 0; hi < 2; ++hi)
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      u32x4_t A;
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj) {
+        const int lo = BITS == 4 ? 8 * ks + jj : 4 * ks + jj, up = lo + (BITS == 4 ? 4 : 8);
+        A[jj] = __builtin_amdgcn_perm(v[up], v[lo], hi ? 0x07060302u : 0x05040100u);
+      }
+      d.v[2 * w + hi][ks][lane] = A;
+    }
+  return __any(bad);
+}
+
+struct WideLds {
+  WideTile tile[2];
+  uint2 szk[4][64];
+  int bad[4];  // a wave met a node's value that is not finite
+};
+
+// S^T = K q^T and O^T += V^T P^T of the tile in LDS.
+__device__ __forceinline__ void wide_scores(const WideTile& d, const RowsQ<2>& Q, f4 (&S)[2][4]) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb) S[t][mb] = f4{0, 0, 0, 0};
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb) {
+      const u32x4_t A = d.k[ks][mb][lane];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) S[t][mb] = mfma_h(A, Q.x[t][ks], S[t][mb]);
+    }
+}
+__device__ __forceinline__ void wide_values(const WideTile& d, const u32x4_t (&P)[2][2],
+                                            RowsState<2>& st) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int cb = 0; cb < 8; ++cb)
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const u32x4_t A = d.v[cb][ks][lane];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) st.o[t][cb] = mfma_h(A, P[t][ks], st.o[t][cb]);
+    }
+}
+
+template <int BITS>
+__device__ __forceinline__ void wide_tiles(const RowsArgs& a, int b, int kh, int head_off,
+                                           const RowsSeq& sq, int j0, int j1, bool work, RowsQ<2>& Q,
+                                           RowsState<2>& st, WideLds& L) {
+  const int w = threadIdx.x >> 6;
+  const long u = (long)b * a.Hkv + kh;
+  const int je = min(j1, sq.nlist);
+  load_q<2, BITS == 4 ? kOrd4 : kOrd2>(a, Q);
+  if (j0 < je) {  // cached groups
+    const int cnt = je - j0;
+    RowsTab T;
+    load_tab<1>(a, b, kh, sq, j0, je, T);
+    WideRaw<BITS> raw;
+    wide_load<BITS>(a, kh, head_off, T, 0, raw);
+    float sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sk), 0));
+    float sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sv), 0));
+    bool live = __builtin_amdgcn_readlane(T.slot, 0) >= 0;
+    wide_expand<BITS>(raw, L.tile[0], L.szk[w]);
+    wide_load<BITS>(a, kh, head_off, T, 1, raw);
+    for (int i = 0; i < cnt; ++i) {
+      __syncthreads();
+      const float ski = sk, svi = sv;
+      const bool livei = live;
+      // the next tile to the other buffer, and its successor's codes requested (past
+      // the end: page 0 and slot 0, expanded to no use)
+      const int at = (i + 1) & 63;
+      sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sk), at));
+      sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sv), at));
+      live = __builtin_amdgcn_readlane(T.slot, at) >= 0;
+      if (at == 63) load_tab<1>(a, b, kh, sq, j0 + i + 2, je, T);
+      wide_expand<BITS>(raw, L.tile[(i + 1) & 1], L.szk[w]);
+      wide_load<BITS>(a, kh, head_off, T, (i + 2) & 63, raw);
+      if (!work || !livei) continue;
+      f4 S[2][4];
+      wide_scores(L.tile[i & 1], Q, S);
+      constexpr float up = 1 << kDown<BITS>;
+      float ex, inv;
+      value_scale(svi, up, ex, inv);
+      u32x4_t P[2][2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        rows_softmax<2, BITS == 4, false>(st, t, S[t], ski * (a.sm_log2e * up), ex, inv, 0, P[t]);
+      wide_values(L.tile[i & 1], P, st);
+    }
+  }
+  // the buffer and the nodes
+  for (int j = max(je, j0); j < j1; ++j) {
+    const bool buffer = j == sq.nlist && sq.nt > 0;
+    const int node = j - sq.nlist - (sq.nt > 0);
+    __syncthreads();
+    if (buffer) {
+      wide_buffer<BITS>(a, u, L.tile[0]);
+    } else {
+      const bool bad = wide_nodes<BITS>(a, u, node, sq.tl, L.tile[0]);
+      if ((threadIdx.x & 63) == 0) L.bad[w] = bad;
+    }
+    __syncthreads();
+    if (!work) continue;
+    f4 S[2][4];
+    wide_scores(L.tile[0], Q, S);
+    float c2 = a.sm_log2e, ex = 0.0f, inv = 1.0f;
+    if (buffer) {
+      c2 *= a.tscale[2 * u];
+      value_scale(a.tscale[2 * u + 1], 1.0f, ex, inv);
+    }
+    u32x4_t P[2][2];
+    unsigned vis[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int g4 = (threadIdx.x & 63) >> 4;
+      vis[t] = buffer ? (1u << min(max(sq.nt - 16 * g4, 0), 16)) - 1u
+                      : nodes_visible(a, b, node, sq.tl, Q.at[t], Q.node[t]);
+      rows_softmax<2, BITS == 4, true>(st, t, S[t], c2, ex, inv, vis[t], P[t]);
+    }
+    wide_values(L.tile[0], P, st);
+    if (!buffer && (L.bad[0] | L.bad[1] | L.bad[2] | L.bad[3]))
+      nodes_nonfinite<2, BITS == 4>(a, a.vt + u * a.T * 128, node, sq.tl, P, vis, st);
+  }
+}
+
+__global__ __launch_bounds__(256, 2) void k_attn_wide(RowsArgs a) {
+  __shared__ __attribute__((aligned(16))) WideLds L;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g4 = lane >> 4;
+  const unsigned span = 8u * a.ntiles_row;  // (the row tiles of a chunk to one XCD)
+  const int rt = (int)(blockIdx.x % span >> 3);
+  int u = (int)(blockIdx.x / span * 8 + (blockIdx.x & 7));
+  const int s = u % a.nchunk;
+  u /= a.nchunk;
+  const int b = u / a.Hkv, kh = u - b * a.Hkv;
+  if (b >= a.B) return;
+  const RowsSeq sq = rows_seq(a, b);
+  const int rows = a.G * sq.tl;
+  if (kWideRows * rt >= rows || s >= max(sq.nparts, 1)) return;
+  const int base = kWideRows * rt + 32 * w;
+  RowsQ<2> Q;
+  RowsState<2> st;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int row = base + 16 * t + n;
+    const int h = row / sq.tl;
+    Q.node[t] = row - h * sq.tl;
+    Q.at[t] = row < rows ? ((long)b * a.Hq + kh * a.G + h) * a.T + Q.node[t] : -1;
+    st.m[t] = -INFINITY;
+    st.l[t] = 0.0f;
+#pragma unroll
+    for (int cb = 0; cb < 8; ++cb) st.o[t][cb] = f4{0, 0, 0, 0};
+  }
+  const int head_off = 512 * (4 * kh - 2 * __popcll(a.int2_mask & ((1ull << kh) - 1ull)));
+  const int j0 = s * sq.len, j1 = min(j0 + sq.len, sq.ntile);
+  const bool work = base < rows;
+  if (j0 < j1) {
+    if ((a.int2_mask >> kh) & 1ull)
+      wide_tiles<2>(a, b, kh, head_off, sq, j0, j1, work, Q, st, L);
+    else
+      wide_tiles<4>(a, b, kh, head_off, sq, j0, j1, work, Q, st, L);
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const float l = add_xor32(st.l[t] + __shfl_xor(st.l[t], 16));
+    if (Q.at[t] < 0) continue;
+    float* ws = a.ws + (Q.at[t] * a.nchunk + s) * kWsStride;
+    if (sq.nparts > 1 && g4 == 0) *reinterpret_cast<float2*>(ws) = make_float2(st.m[t], l);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int c0 = 32 * g4 + 8 * r;
+      const float o[8] = {st.o[t][0][r], st.o[t][1][r], st.o[t][2][r], st.o[t][3][r],
+                          st.o[t][4][r], st.o[t][5][r], st.o[t][6][r], st.o[t][7][r]};
+      if (sq.nparts <= 1) {
+        rows_store(a, Q.at[t], c0, st.m[t], l, o);
+      } else {
+        *reinterpret_cast<float4*>(ws + kWsO + c0) = make_float4(o[0], o[1], o[2], o[3]);
+        *reinterpret_cast<float4*>(ws + kWsO + c0 + 4) = make_float4(o[4], o[5], o[6], o[7]);
+      }
+    }
+  }
+}
+
 // Rows of several chunks: a wave merges a row's states, a quarter of them in each 16
 // lanes (four at a time, their loads together), then the quarters.
 __global__ __launch_bounds__(256) void k_rows_merge(RowsArgs a) {
@@ -816,16 +1185,18 @@ __global__ __launch_bounds__(256) void k_rows_merge(RowsArgs a) {
   if (lane < 16) rows_store(a, at, c0, m, l, o);
 }
 
-// Tiles of 16 query rows that a wave takes: a second one shares the codes' expansion.
-inline int rows_nt(int G, int T) { return G * T <= 16 ? 1 : 2; }
-inline int rows_tiles_per_head(int G, int T) { return ceil_div(G * T, 16 * rows_nt(G, T)); }
+// Query rows of a work-group: one or two tiles of 16 for every wave (the second shares
+// the codes' expansion), or 128 between them.
+inline int rows_tile(int G, int T) { return G * T <= 16 ? 16 : (G * T <= 64 ? 32 : kWideRows); }
+inline int rows_tiles_per_head(int G, int T) { return ceil_div(G * T, rows_tile(G, T)); }
+// Tiles of a chunk, at least: one a wave where the waves take tiles in turn.
+inline int rows_min_len(int G, int T) { return rows_tile(G, T) == kWideRows ? 8 : kRowsWaves; }
 
-// Chunks of the grid: as many as give the GPU two work-groups per CU, each with at
-// least one tile per wave.
+// Chunks of the grid: as many as give the GPU two work-groups per CU.
 inline int rows_chunks(int B, int Hkv, int G, int T, int max_tiles) {
   const long units = (long)B * Hkv * rows_tiles_per_head(G, T);
   const long want = (512 + units - 1) / units;
-  const long most = ceil_div(max_tiles, kRowsWaves);
+  const long most = ceil_div(max_tiles, rows_min_len(G, T));
   return (int)(want < most ? (want > 1 ? want : 1) : (most > 1 ? most : 1));
 }
 
@@ -835,10 +1206,13 @@ inline long rows_groups(const RowsArgs& a) {
 
 inline hipError_t launch_attn_rows(const RowsArgs& a, hipStream_t stream) {
   const dim3 groups((unsigned)rows_groups(a)), threads(64 * kRowsWaves);
-  if (rows_nt(a.G, a.T) == 1)
+  const int tile = rows_tile(a.G, a.T);
+  if (tile == 16)
     hipLaunchKernelGGL((k_attn_rows<1>), groups, threads, 0, stream, a);
-  else
+  else if (tile == 32)
     hipLaunchKernelGGL((k_attn_rows<2>), groups, threads, 0, stream, a);
+  else
+    hipLaunchKernelGGL(k_attn_wide, groups, threads, 0, stream, a);
   if (a.nchunk > 1) {
     const long rows = (long)a.B * a.Hq * a.T;
     hipLaunchKernelGGL(k_rows_merge, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a);

@@ -86,6 +86,9 @@ TREES = [
     (2, 4, 2, [2, 4], [64 * 12 + 1, 30], 65, [65, 64], "any", True),
     (1, 8, 1, [4], [64 * 21 + 40], 129, [129], "chain", True),
     (2, 4, 4, [4, 2, 2, 4], [64 * 4 + 9, 64 * 130], 256, [256, 200], "tree", True),
+    (1, 4, 1, [2], [64 * 140 + 9], 30, [30], "tree", True),     # past 64 table entries
+    (1, 2, 1, [4], [64 * 66], 64, [64], "any", False),
+    (2, 16, 1, [4], [64 * 4 + 2, 64 * 17], 8, [8, 5], "tree", True),
     (9, 8, 8, [4, 2] * 4, [64 * i + 7 * i for i in range(9)], 4, [4, 3, 2, 1, 0, 4, 4, 4, 4], "tree", True),
 ]
 
@@ -128,23 +131,23 @@ def test_tree_ranges(ta, dev, scale, sm):
     _check_tree(f, q, kt, vt, see, [T], o, lse, sm=sm)
 
 
-def test_tree_rows_do_not_see_what_their_mask_hides(ta, dev):
+@pytest.mark.parametrize("Hq,T,tl", [(4, 70, [66, 40]), (2, 40, [40, 35]), (2, 16, [16, 9])])
+def test_tree_rows_do_not_see_what_their_mask_hides(ta, dev, Hq, T, tl):
     """Infinities and NaN in nodes a row does not see, and behind the tree's last,
     change nothing; in nodes it sees they do what the formula does."""
-    B, Hq, Hkv, T = 2, 4, 2, 70
-    tl = [66, 40]
+    B, Hkv = 2, 2
     f = ref.Filled(ta, dev, [64 * 3 + 20, 64 * 8], [4, 2], seed=41)
     q, kt, vt = ref.rand((B, Hq, T, D), 1), ref.rand((B, Hkv, T, D), 2), ref.rand((B, Hkv, T, D), 3)
     see = _trees("tree", B, T, tl, 5)
-    hidden = np.zeros(T, bool)
-    hidden[[3, 17, 33, 64]] = True
+    hidden = [i for i in (0, 3, 8, 17, 33, 64) if i < T]
     see[:, :, hidden] = False
     clean = [x.clone() for x in (kt, vt)]
+    bad = [float("nan"), float("inf"), float("-inf")]
+    for i, h in enumerate(hidden):
+        kt[:, :, h], vt[:, :, h] = bad[i % 3], bad[(i + 1) % 3]
     for b in range(B):
         kt[b, :, tl[b]:] = float("nan")
         vt[b, :, tl[b]:] = float("inf")
-    kt[:, :, 3], kt[:, :, 17], kt[:, :, 33] = float("nan"), float("inf"), float("-inf")
-    vt[:, :, 3], vt[:, :, 17], vt[:, :, 64] = float("nan"), float("inf"), float("-inf")
     tld = torch.tensor(tl, dtype=torch.int32, device=dev)
 
     def run(k, v, m):
@@ -157,16 +160,21 @@ def test_tree_rows_do_not_see_what_their_mask_hides(ta, dev):
     a, b_ = run(kt, vt, see), run(*clean, see)
     assert torch.equal(a[0].view(torch.int16), b_[0].view(torch.int16)) and torch.equal(a[1], b_[1])
     # node 2 sees an infinite value, node 5 one that is not a number, node 6 such a key
-    seen = see.copy()
-    seen[:, 2, 17], seen[:, 5, 3], seen[:, 6, 33] = True, True, True
-    k2, v2 = clean[0].clone(), clean[1].clone()
-    v2[:, :, 17, 5], v2[:, :, 3, 9], k2[:, :, 33] = float("inf"), float("nan"), float("nan")
-    o, lse = run(k2, v2, seen)
-    assert torch.isinf(o[:, :, 2, 5]).all() and torch.isfinite(o[:, :, 2, 6]).all()
-    assert torch.isnan(o[:, :, 5, 9]).all() and torch.isfinite(o[:, :, 5, 8]).all()
-    assert torch.isnan(o[:, :, 6]).all() and torch.isnan(lse[:, :, 6]).all()
-    rest = [i for i in range(T) if i not in (2, 5, 6)]
-    assert torch.equal(o[:, :, rest].view(torch.int16), b_[0][:, :, rest].view(torch.int16))
+    for far in (h for h in hidden if h < min(tl)):
+        seen = see.copy()
+        seen[:, 2, far], seen[:, 5, far], seen[:, 6, far] = True, True, True
+        for which, row, value in (("v", 2, float("inf")), ("v", 5, float("nan")), ("k", 6, float("nan"))):
+            k2, v2 = clean[0].clone(), clean[1].clone()
+            (v2 if which == "v" else k2)[:, :, far, 5] = value
+            o, lse = run(k2, v2, seen)
+            cut = [i for i in range(T) if i not in (2, 5, 6)]
+            assert torch.equal(o[:, :, cut].view(torch.int16), b_[0][:, :, cut].view(torch.int16))
+            if which == "k":
+                assert torch.isnan(o[:, :, row]).all() and torch.isnan(lse[:, :, row]).all()
+            else:
+                x = o[:, :, row, 5]
+                assert (torch.isnan(x) if value != value else torch.isinf(x)).all()
+                assert torch.isfinite(o[:, :, row, 6:]).all() and torch.isfinite(o[:, :, row, :5]).all()
 
 
 def test_tree_large_finite_values(ta, dev):
