@@ -23,12 +23,12 @@
 // wave takes 16 of them and a tile:
 //   S^T = K q^T   (16x16x32 fp16 MFMA; A row m of block mb: token
 //                  16 (m >> 2) + 4 mb + (m & 3) of the tile)
-//   O^T += V^T P^T (A row m of block cb: channel 8 m + cb)
+//   O^T += V^T P^T (A row m of block cb: channel 32 (cb >> 1) + 2 m + (cb & 1))
 // With this order of tokens lane (n, g4) -- n = lane & 15 the query row, g4 =
 // lane >> 4 -- holds the scores of the 16 tokens of page g4, which are the ones
 // its operand of the second product needs: P never leaves the registers, and the
-// row's m and l are the lane's own.  With this order of channels a lane's codes of
-// V are one run of its page, and its outputs runs of 8 channels.
+// row's m and l are the lane's own.  With this order of channels the lanes' codes of V
+// are contiguous in every load, and a lane's outputs runs of 8 channels.
 #include "turbo_common.h"
 #include "stream_loads.h"
 
@@ -38,6 +38,7 @@ typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 // q, the nodes' keys and values and o may lie at any fp16 boundary
 typedef unsigned u4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned u1_any __attribute__((aligned(2)));
 
 struct RowsArgs {
   const unsigned short* q;   // fp16 [B][Hq][T][128]
@@ -65,7 +66,7 @@ struct RowsArgs {
   const float* tscale;
   int ntiles_row;            // row tiles in the grid
   int nchunk;                // chunks in the grid
-  int min_len;               // tiles of a chunk, at least
+  int len;                   // tiles of a chunk
   float* ws;                 // [B][Hq][T][nchunk][132]: m, l, -, -, O[128]
   unsigned short* o;         // fp16 [B][Hq][T][128]
   float* lse;                // [B][Hq][T] or null
@@ -93,9 +94,24 @@ __device__ __forceinline__ RowsSeq rows_seq(const RowsArgs& a, int b) {
   s.tl = a.tree_lens ? min(max(a.tree_lens[b], 0), a.T) : a.T;
   s.nlist = a.sel ? a.nsel : s.ng;
   s.ntile = s.nlist + (s.nt > 0) + (a.kt ? (s.tl + 63) / 64 : 0);
-  s.len = max(a.min_len, ceil_div(s.ntile, a.nchunk));
+  s.len = a.len;
   s.nparts = ceil_div(s.ntile, s.len);
   return s;
+}
+
+// The work of a work-group; false past the last.  They go to the eight XCDs in turn:
+// the row tiles of a chunk, which read the same codes, to one of them.  The first
+// chunks of all heads come first, the second ones after them: the chunks that short
+// sequences do not have lie together, not on some of the XCDs.
+__device__ __forceinline__ bool rows_place(const RowsArgs& a, int& b, int& kh, int& s, int& rt) {
+  const unsigned span = 8u * a.ntiles_row;
+  rt = (int)(blockIdx.x % span >> 3);
+  const int u = (int)(blockIdx.x / span * 8 + (blockIdx.x & 7));
+  s = u / (a.B * a.Hkv);
+  const int bh = u - s * (a.B * a.Hkv);
+  b = bh / a.Hkv;
+  kh = bh - b * a.Hkv;
+  return s < a.nchunk;
 }
 
 __device__ __forceinline__ f4 mfma_h(u32x4_t a, u32x4_t b, f4 c) {
@@ -215,7 +231,8 @@ __device__ __forceinline__ void load_q(const RowsArgs& a, RowsQ<NT>& Q) {
   }
 }
 
-// Running state of the wave's rows: O^T (channel 32 g4 + 8 r + cb in O[t][cb][r]),
+// Running state of the wave's rows: O^T (channel 32 e + 8 g4 + 2 r + hi in
+// o[t][2 e + hi][r]),
 // maximum (in units of log2) and this lane's part of the sum.
 template <int NT>
 struct RowsState {
@@ -328,9 +345,9 @@ __device__ __forceinline__ void load_tab(const RowsArgs& a, int b, int kh, const
 template <int BITS>
 struct RowsGroup {
   unsigned k[4][BITS];     // codes of token (m, mb), the lane's 32 channels
-  unsigned v[8 * BITS / 2];  // codes of channels 8 n .. 8 n + 7, the lane's page
+  unsigned v[8 * BITS / 2];  // codes of channels 32 e + 2 n and + 1, the lane's page
   uint2 ks, kz;            // s^int, z^int of the 8 channels that hold the lane's pair
-  uint2 vs, vz;            // of channels 8 n .. 8 n + 7
+  unsigned vs, vz;         // of channels 2 lane and + 1
 };
 
 // K and V of the i-th tile of T.  One with nothing to attend loads page 0 and slot 0,
@@ -376,15 +393,20 @@ template <int BITS>
 __device__ __forceinline__ void load_group_v(const RowsArgs& a, int kh, int head_off, const RowsTab& T,
                                              int i, RowsGroup<BITS>& x) {
   const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
-  const uint8_t* vp = a.pages + tab_page(a, T, i, g4) + head_off + 256 * BITS + n * 16 * BITS;
+  const uint8_t* vp = a.pages + tab_page(a, T, i, g4) + head_off + 256 * BITS + n * 4 * BITS;
 #pragma unroll
-  for (int e = 0; e < BITS; ++e) {
-    const u32x4_t w = load_nt4(vp + 16 * e);
-    x.v[4 * e] = w.x; x.v[4 * e + 1] = w.y; x.v[4 * e + 2] = w.z; x.v[4 * e + 3] = w.w;
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (BITS == 4) {
+      const u32x4_t w = load_nt4(vp + 256 * e);
+      x.v[4 * e] = w.x; x.v[4 * e + 1] = w.y; x.v[4 * e + 2] = w.z; x.v[4 * e + 3] = w.w;
+    } else {
+      const u32x2_t w = load_nt2(vp + 128 * e);
+      x.v[2 * e] = w.x; x.v[2 * e + 1] = w.y;
+    }
   }
   const int8_t* meta = tab_meta(a, T, i, kh);
-  x.vs = *reinterpret_cast<const uint2*>(meta + 256 + 8 * n);
-  x.vz = *reinterpret_cast<const uint2*>(meta + 384 + 8 * n);
+  x.vs = *reinterpret_cast<const unsigned short*>(meta + 256 + 2 * lane);
+  x.vz = *reinterpret_cast<const unsigned short*>(meta + 384 + 2 * lane);
 }
 
 // S^T = K q^T of a group.
@@ -428,13 +450,19 @@ __device__ __forceinline__ void group_scores(const RowsGroup<BITS>& x, const Row
 // O^T += V^T P^T of a group.
 template <int BITS, int NT>
 __device__ __forceinline__ void group_values(const RowsGroup<BITS>& x, const u32x4_t (&P)[NT][2],
-                                             RowsState<NT>& st) {
+                                             RowsState<NT>& st, uint4* szv) {
+  const int lane = threadIdx.x & 63, n = lane & 15;
+  {  // factors and zero points of channel pairs, one a lane, exchanged through LDS
+    const unsigned s = scale_h2(__builtin_amdgcn_perm(0u, x.vs, 0x0c010c00u));
+    const unsigned z = zero_h2(__builtin_amdgcn_perm(0u, x.vz, 0x0c010c00u));
+    wave_sync();
+    szv[lane] = make_uint4(scale_at<BITS>(s, 0), scale_at<BITS>(s, 1), zero_at<BITS>(z), 0u);
+    wave_sync();
+  }
 #pragma unroll
-  for (int c2 = 0; c2 < 4; ++c2) {  // channels 8 n + 2 c2 and + 1
-    const unsigned sel = c2 & 1 ? 0x0c030c02u : 0x0c010c00u;
-    const unsigned s = scale_h2(__builtin_amdgcn_perm(0u, c2 < 2 ? x.vs.x : x.vs.y, sel));
-    const unsigned z = zero_h2(__builtin_amdgcn_perm(0u, c2 < 2 ? x.vz.x : x.vz.y, sel));
-    const unsigned s0 = scale_at<BITS>(s, 0), s1 = scale_at<BITS>(s, 1), zd = zero_at<BITS>(z);
+  for (int c2 = 0; c2 < 4; ++c2) {  // channels 32 c2 + 2 n and + 1
+    const uint4 sz = szv[16 * c2 + n];
+    const unsigned s0 = sz.x, s1 = sz.y, zd = sz.z;
 #pragma unroll
     for (int hi = 0; hi < 2; ++hi) {
       const int cb = 2 * c2 + hi;
@@ -489,7 +517,7 @@ __device__ __forceinline__ void step_buffer(const RowsArgs& a, long u, int nt, c
     rows_softmax<NT, true, true>(st, t, S[t], sk * a.sm_log2e, ex, inv, (1u << live) - 1u, P[t]);
 #pragma unroll
   for (int cb = 0; cb < 8; ++cb) {
-    const int8_t* vr = a.tv + (u * 128 + 8 * n + cb) * 64 + 16 * g4;
+    const int8_t* vr = a.tv + (u * 128 + 32 * (cb >> 1) + 2 * n + (cb & 1)) * 64 + 16 * g4;
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       const unsigned w0 = reinterpret_cast<const unsigned*>(vr)[2 * ks] ^ 0x80808080u;
@@ -535,7 +563,7 @@ __device__ void nodes_nonfinite(const RowsArgs& a, const unsigned short* vb, int
   const int lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
   const int cnt = min(tl - 64 * j, 64);
   for (int i = 0; i < cnt; ++i) {
-    const unsigned short* vr = vb + (64L * j + i) * 128 + 32 * g4;
+    const unsigned short* vr = vb + (64L * j + i) * 128 + 8 * g4;
     const int from = 16 * (i >> 4) + n;  // lane that holds the row's p of token i
     // register (ks, jj) and half of token i & 15 of the page
     const int tok = i & 15;
@@ -555,7 +583,7 @@ __device__ void nodes_nonfinite(const RowsArgs& a, const unsigned short* vb, int
       for (int cb = 0; cb < 8; ++cb)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const unsigned short x = vr[8 * r + cb];
+          const unsigned short x = vr[32 * (cb >> 1) + 2 * r + (cb & 1)];
           if ((x & 0x7c00u) == 0x7c00u) st.o[t][cb][r] += p * (float)__builtin_bit_cast(_Float16, x);
         }
     }
@@ -596,16 +624,15 @@ __device__ __forceinline__ void step_nodes(const RowsArgs& a, int b, long u, int
   bool bad = false;
 #pragma unroll
   for (int ks = 0; ks < 2; ++ks) {
-    unsigned v[8][4];  // token 8 ks + i of the page, channels 8 n .. 8 n + 7
+    unsigned v[8][4];  // token 8 ks + i of the page, channels 32 e + 2 n and + 1
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int tok = 64 * j + 16 * g4 + 8 * ks + i;
-      u4_any x = {0, 0, 0, 0};
-      if (tok < tl) x = *reinterpret_cast<const u4_any*>(vb + (long)tok * 128 + 8 * n);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        bad = bad || nonfinite_h2(x[e]);
-        v[i][e] = x[e];
+        v[i][e] = 0u;
+        if (tok < tl) v[i][e] = *reinterpret_cast<const u1_any*>(vb + (long)tok * 128 + 32 * e + 2 * n);
+        bad = bad || nonfinite_h2(v[i][e]);
       }
     }
     if (__any(bad)) {
@@ -662,7 +689,7 @@ constexpr int kRowsLds = 132;  // floats of a row's state in LDS
 template <int BITS, int NT>
 __device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int head_off,
                                            const RowsSeq& sq, int j0, int j1, RowsQ<NT>& Q,
-                                           RowsState<NT>& st, uint2* szk) {
+                                           RowsState<NT>& st, uint2* szk, uint4* szv) {
   const int w = threadIdx.x >> 6;
   const long u = (long)b * a.Hkv + kh;
   int j = j0 + w;
@@ -693,7 +720,7 @@ __device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int
 #pragma unroll
         for (int t = 0; t < NT; ++t)
           rows_softmax<NT, BITS == 4, false>(st, t, S[t], sk * (a.sm_log2e * up), ex, inv, 0, P[t]);
-        group_values<BITS, NT>(x, P, st);
+        group_values<BITS, NT>(x, P, st, szv);
       }
       load_group_v<BITS>(a, kh, head_off, T, (i + 1) & 63, x);
     }
@@ -715,16 +742,10 @@ template <int NT>
 __global__ __launch_bounds__(64 * kRowsWaves) void k_attn_rows(RowsArgs a) {
   __shared__ __attribute__((aligned(16))) float part[kRowsWaves][16][kRowsLds];
   __shared__ uint2 szk[kRowsWaves][64];
+  __shared__ uint4 szv[kRowsWaves][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g4 = lane >> 4;
-  // work-groups go to the eight XCDs in turn: the row tiles of a chunk, which read the
-  // same codes, to one of them
-  const unsigned span = 8u * a.ntiles_row;
-  const int rt = (int)(blockIdx.x % span >> 3);
-  int u = (int)(blockIdx.x / span * 8 + (blockIdx.x & 7));
-  const int s = u % a.nchunk;
-  u /= a.nchunk;
-  const int b = u / a.Hkv, kh = u - b * a.Hkv;
-  if (b >= a.B) return;
+  int b, kh, s, rt;
+  if (!rows_place(a, b, kh, s, rt)) return;
   const RowsSeq sq = rows_seq(a, b);
   const int base = 16 * NT * rt, rows = a.G * sq.tl;
   if (base >= rows || s >= max(sq.nparts, 1)) return;
@@ -744,9 +765,9 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_attn_rows(RowsArgs a) {
   const int head_off = 512 * (4 * kh - 2 * __popcll(a.int2_mask & ((1ull << kh) - 1ull)));
   const int j0 = s * sq.len, j1 = min(j0 + sq.len, sq.ntile);
   if ((a.int2_mask >> kh) & 1ull)
-    rows_tiles<2, NT>(a, b, kh, head_off, sq, j0, j1, Q, st, szk[w]);
+    rows_tiles<2, NT>(a, b, kh, head_off, sq, j0, j1, Q, st, szk[w], szv[w]);
   else
-    rows_tiles<4, NT>(a, b, kh, head_off, sq, j0, j1, Q, st, szk[w]);
+    rows_tiles<4, NT>(a, b, kh, head_off, sq, j0, j1, Q, st, szk[w], szv[w]);
   // the waves' states to LDS, and their merge: 16 lanes a row
   const int row = threadIdx.x >> 4, c0 = 8 * (threadIdx.x & 15);
 #pragma unroll
@@ -756,10 +777,11 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_attn_rows(RowsArgs a) {
     if (t > 0) __syncthreads();
     if (g4 == 0) *reinterpret_cast<float2*>(p) = make_float2(st.m[t], l);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float* d = p + 4 + 32 * g4 + 8 * r;
-      *reinterpret_cast<f4*>(d) = f4{st.o[t][0][r], st.o[t][1][r], st.o[t][2][r], st.o[t][3][r]};
-      *reinterpret_cast<f4*>(d + 4) = f4{st.o[t][4][r], st.o[t][5][r], st.o[t][6][r], st.o[t][7][r]};
+    for (int e = 0; e < 4; ++e) {
+      const f4 x = st.o[t][2 * e], y = st.o[t][2 * e + 1];
+      float* d = p + 4 + 32 * e + 8 * g4;
+      *reinterpret_cast<f4*>(d) = f4{x[0], y[0], x[1], y[1]};
+      *reinterpret_cast<f4*>(d + 4) = f4{x[2], y[2], x[3], y[3]};
     }
     __syncthreads();
     const int at_row = base + 16 * t + row;
@@ -794,38 +816,47 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_attn_rows(RowsArgs a) {
 // instructions for 16 rows, is shared: the four waves of a work-group take 32 rows
 // each, expand a quarter of the next tile into LDS, in the order in which its lanes
 // hold the operands, and read all of this one.  Two buffers, one barrier a tile.
-constexpr int kWideRows = 128;
+template <int NW>
+constexpr int kWideRows = 32 * NW;
 
 struct WideTile {
   u32x4_t k[4][4][64];  // [ks][mb][lane]
   u32x4_t v[8][2][64];  // [cb][ks][lane]
 };
 
-template <int BITS>
+// What a wave expands of a tile: of K, m-block w & 3, all four k-steps (NW = 4) or two
+// of them; of V, channels 32 w + 2 n and + 1, or one of those of w >> 1.
+template <int BITS, int NW>
 struct WideRaw {
-  unsigned k[BITS];     // codes of token (m, mb = wave)
-  unsigned v[BITS];     // codes of channels 8 n + 2 wave, + 1, the lane's page
+  static constexpr int kWords = BITS * 4 / NW;
+  unsigned k[kWords], v[kWords];
   uint2 ks, kz;
-  unsigned vs, vz;      // s^int, z^int of the two channels, low bytes
+  unsigned vs, vz;  // s^int, z^int of the channels in bits 0-7 (and 8-15)
 };
 
-template <int BITS>
-__device__ __forceinline__ void wide_load(const RowsArgs& a, int kh, int head_off, const RowsTab& T,
-                                          int i, WideRaw<BITS>& x) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g4 = lane >> 4;
-  const uint8_t* kp = a.pages + tab_page(a, T, i, n >> 2) + head_off +
-                      (4 * w + (n & 3)) * 16 * BITS + 4 * BITS * g4;
-  const uint8_t* vp =
-      a.pages + tab_page(a, T, i, g4) + head_off + 256 * BITS + n * 16 * BITS + 4 * BITS * w;
-  if constexpr (BITS == 4) {
-    const uint4 c = *reinterpret_cast<const uint4*>(kp), d = *reinterpret_cast<const uint4*>(vp);
-    x.k[0] = c.x; x.k[1] = c.y; x.k[2] = c.z; x.k[3] = c.w;
-    x.v[0] = d.x; x.v[1] = d.y; x.v[2] = d.z; x.v[3] = d.w;
+template <int WORDS>
+__device__ __forceinline__ void load_words(const uint8_t* p, unsigned (&x)[WORDS]) {
+  if constexpr (WORDS == 4) {
+    const uint4 c = *reinterpret_cast<const uint4*>(p);
+    x[0] = c.x; x[1] = c.y; x[2] = c.z; x[3] = c.w;
+  } else if constexpr (WORDS == 2) {
+    const uint2 c = *reinterpret_cast<const uint2*>(p);
+    x[0] = c.x; x[1] = c.y;
   } else {
-    const uint2 c = *reinterpret_cast<const uint2*>(kp), d = *reinterpret_cast<const uint2*>(vp);
-    x.k[0] = c.x; x.k[1] = c.y;
-    x.v[0] = d.x; x.v[1] = d.y;
+    x[0] = *reinterpret_cast<const unsigned*>(p);
   }
+}
+
+template <int BITS, int NW>
+__device__ __forceinline__ void wide_load(const RowsArgs& a, int kh, int head_off, const RowsTab& T,
+                                          int i, WideRaw<BITS, NW>& x) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g4 = lane >> 4;
+  load_words(a.pages + tab_page(a, T, i, n >> 2) + head_off + (4 * (w & 3) + (n & 3)) * 16 * BITS +
+                 4 * BITS * g4 + 2 * BITS * (w >> 2),
+             x.k);
+  load_words(a.pages + tab_page(a, T, i, g4) + head_off + 256 * BITS +
+                 (NW == 4 ? (32 * w + 2 * n) : (32 * (w >> 1) + 2 * n + (w & 1))) * 2 * BITS,
+             x.v);
   constexpr int ORD = BITS == 4 ? kOrd4 : kOrd2;
   const int8_t* meta = tab_meta(a, T, i, kh);
   const int8_t* mk = meta + 32 * g4 + (chan_lo<ORD>(n >> 2, n & 3) & ~3);
@@ -833,12 +864,17 @@ __device__ __forceinline__ void wide_load(const RowsArgs& a, int kh, int head_of
                     *reinterpret_cast<const unsigned*>(mk + kChanDist<ORD>));
   x.kz = make_uint2(*reinterpret_cast<const unsigned*>(mk + 128),
                     *reinterpret_cast<const unsigned*>(mk + 128 + kChanDist<ORD>));
-  x.vs = *reinterpret_cast<const unsigned short*>(meta + 256 + 8 * n + 2 * w);
-  x.vz = *reinterpret_cast<const unsigned short*>(meta + 384 + 8 * n + 2 * w);
+  if constexpr (NW == 4) {
+    x.vs = *reinterpret_cast<const unsigned short*>(meta + 256 + 32 * w + 2 * n);
+    x.vz = *reinterpret_cast<const unsigned short*>(meta + 384 + 32 * w + 2 * n);
+  } else {
+    x.vs = *reinterpret_cast<const unsigned char*>(meta + 256 + 32 * (w >> 1) + 2 * n + (w & 1));
+    x.vz = *reinterpret_cast<const unsigned char*>(meta + 384 + 32 * (w >> 1) + 2 * n + (w & 1));
+  }
 }
 
-template <int BITS>
-__device__ __forceinline__ void wide_expand(const WideRaw<BITS>& x, WideTile& d, uint2* szk) {
+template <int BITS, int NW>
+__device__ __forceinline__ void wide_expand(const WideRaw<BITS, NW>& x, WideTile& d, uint2* szk) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g4 = lane >> 4;
   {
     const int sh = 8 * (n & 3);
@@ -848,23 +884,25 @@ __device__ __forceinline__ void wide_expand(const WideRaw<BITS>& x, WideTile& d,
     szk[lane] = make_uint2(n & 1 ? scale_at<BITS>(s, 1) : scale_at<BITS>(s, 0), zero_at<BITS>(z));
     wave_sync();
   }
+  const int k0 = NW == 4 ? 0 : 2 * (w >> 2);
 #pragma unroll
-  for (int ks = 0; ks < 4; ++ks) {
+  for (int kk = 0; kk < 16 / NW; ++kk) {
     u32x4_t A;
 #pragma unroll
     for (int jj = 0; jj < 4; ++jj) {
-      const uint2 sz = szk[16 * g4 + 4 * ks + jj];
-      const unsigned c = BITS == 4 ? code_pair<BITS>(x.k[ks], jj)
-                                   : code_pair<BITS>(x.k[ks >> 1], 4 * (ks & 1) + jj);
+      const uint2 sz = szk[16 * g4 + 4 * (k0 + kk) + jj];
+      const unsigned c = BITS == 4 ? code_pair<BITS>(x.k[kk], jj)
+                                   : code_pair<BITS>(x.k[kk >> 1], 4 * (kk & 1) + jj);
       A[jj] = h2_fma(c, sz.x, sz.y);
     }
-    d.k[ks][w][lane] = A;
+    d.k[k0 + kk][w & 3][lane] = A;
   }
-  const unsigned s = scale_h2(__builtin_amdgcn_perm(0u, x.vs, 0x0c010c00u));
-  const unsigned z = zero_h2(__builtin_amdgcn_perm(0u, x.vz, 0x0c010c00u));
+  const unsigned pick = NW == 4 ? 0x0c010c00u : 0x0c000c00u;
+  const unsigned s = scale_h2(__builtin_amdgcn_perm(0u, x.vs, pick));
+  const unsigned z = zero_h2(__builtin_amdgcn_perm(0u, x.vz, pick));
   const unsigned s0 = scale_at<BITS>(s, 0), s1 = scale_at<BITS>(s, 1), zd = zero_at<BITS>(z);
 #pragma unroll
-  for (int hi = 0; hi < 2; ++hi)
+  for (int hi = 0; hi < 8 / NW; ++hi)
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       u32x4_t A;
@@ -874,7 +912,7 @@ __device__ __forceinline__ void wide_expand(const WideRaw<BITS>& x, WideTile& d,
                                      : code_pair<BITS>(x.v[hi], 4 * ks + jj);
         A[jj] = h2_fma(c, h2_splat(jj & 1 ? s1 : s0, hi), h2_splat(zd, hi));
       }
-      d.v[2 * w + hi][ks][lane] = A;
+      d.v[8 / NW * w + hi][ks][lane] = A;
     }
 }
 
@@ -900,7 +938,7 @@ __device__ __forceinline__ void wide_buffer(const RowsArgs& a, long u, WideTile&
   }
 #pragma unroll
   for (int hi = 0; hi < 2; ++hi) {
-    const int8_t* vr = a.tv + (u * 128 + 8 * n + 2 * w + hi) * 64 + 16 * g4;
+    const int8_t* vr = a.tv + (u * 128 + 32 * w + 2 * n + hi) * 64 + 16 * g4;
     unsigned vw[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) vw[i] = reinterpret_cast<const unsigned*>(vr)[i] ^ 0x80808080u;
@@ -941,13 +979,12 @@ __device__ __forceinline__ bool wide_nodes(const RowsArgs& a, long u, int j, int
     }
     d.k[ks][w][lane] = A;
   }
-  typedef unsigned u1_any __attribute__((aligned(2)));
   unsigned v[16];
   bool bad = false;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const int t = 64 * j + 16 * g4 + i;
-    v[i] = t < tl ? *reinterpret_cast<const u1_any*>(a.vt + (u * a.T + t) * 128 + 8 * n + 2 * w) : 0u;
+    v[i] = t < tl ? *reinterpret_cast<const u1_any*>(a.vt + (u * a.T + t) * 128 + 32 * w + 2 * n) : 0u;
     bad = bad || nonfinite_h2(v[i]);
     if ((v[i] & 0x7c00u) == 0x7c00u) v[i] &= 0xffff0000u;
     if ((v[i] & 0x7c000000u) == 0x7c000000u) v[i] &= 0xffffu;
@@ -967,11 +1004,25 @@ __device__ __forceinline__ bool wide_nodes(const RowsArgs& a, long u, int j, int
   return __any(bad);
 }
 
+template <int NW>
 struct WideLds {
   WideTile tile[2];
-  uint2 szk[4][64];
+  uint2 szk[NW][64];
   int bad[4];  // a wave met a node's value that is not finite
 };
+
+// Order of a block of 16 fragment reads from LDS and the 32 matrix instructions they
+// feed: four reads ahead of every eight instructions (128 cycles, about a read's
+// latency).  Left alone, the compiler reads each fragment right before its use.
+__device__ __forceinline__ void wide_order() {
+  __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+}
 
 // S^T = K q^T and O^T += V^T P^T of the tile in LDS.
 __device__ __forceinline__ void wide_scores(const WideTile& d, const RowsQ<2>& Q, f4 (&S)[2][4]) {
@@ -988,6 +1039,7 @@ __device__ __forceinline__ void wide_scores(const WideTile& d, const RowsQ<2>& Q
 #pragma unroll
       for (int t = 0; t < 2; ++t) S[t][mb] = mfma_h(A, Q.x[t][ks], S[t][mb]);
     }
+  wide_order();
 }
 __device__ __forceinline__ void wide_values(const WideTile& d, const u32x4_t (&P)[2][2],
                                             RowsState<2>& st) {
@@ -1000,12 +1052,13 @@ __device__ __forceinline__ void wide_values(const WideTile& d, const u32x4_t (&P
 #pragma unroll
       for (int t = 0; t < 2; ++t) st.o[t][cb] = mfma_h(A, P[t][ks], st.o[t][cb]);
     }
+  wide_order();
 }
 
-template <int BITS>
+template <int BITS, int NW>
 __device__ __forceinline__ void wide_tiles(const RowsArgs& a, int b, int kh, int head_off,
                                            const RowsSeq& sq, int j0, int j1, bool work, RowsQ<2>& Q,
-                                           RowsState<2>& st, WideLds& L) {
+                                           RowsState<2>& st, WideLds<NW>& L) {
   const int w = threadIdx.x >> 6;
   const long u = (long)b * a.Hkv + kh;
   const int je = min(j1, sq.nlist);
@@ -1014,13 +1067,13 @@ __device__ __forceinline__ void wide_tiles(const RowsArgs& a, int b, int kh, int
     const int cnt = je - j0;
     RowsTab T;
     load_tab<1>(a, b, kh, sq, j0, je, T);
-    WideRaw<BITS> raw;
-    wide_load<BITS>(a, kh, head_off, T, 0, raw);
+    WideRaw<BITS, NW> raw;
+    wide_load<BITS, NW>(a, kh, head_off, T, 0, raw);
     float sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sk), 0));
     float sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sv), 0));
     bool live = __builtin_amdgcn_readlane(T.slot, 0) >= 0;
-    wide_expand<BITS>(raw, L.tile[0], L.szk[w]);
-    wide_load<BITS>(a, kh, head_off, T, 1, raw);
+    wide_expand<BITS, NW>(raw, L.tile[0], L.szk[w]);
+    wide_load<BITS, NW>(a, kh, head_off, T, 1, raw);
     for (int i = 0; i < cnt; ++i) {
       __syncthreads();
       const float ski = sk, svi = sv;
@@ -1032,8 +1085,8 @@ __device__ __forceinline__ void wide_tiles(const RowsArgs& a, int b, int kh, int
       sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sv), at));
       live = __builtin_amdgcn_readlane(T.slot, at) >= 0;
       if (at == 63) load_tab<1>(a, b, kh, sq, j0 + i + 2, je, T);
-      wide_expand<BITS>(raw, L.tile[(i + 1) & 1], L.szk[w]);
-      wide_load<BITS>(a, kh, head_off, T, (i + 2) & 63, raw);
+      wide_expand<BITS, NW>(raw, L.tile[(i + 1) & 1], L.szk[w]);
+      wide_load<BITS, NW>(a, kh, head_off, T, (i + 2) & 63, raw);
       if (!work || !livei) continue;
       f4 S[2][4];
       wide_scores(L.tile[i & 1], Q, S);
@@ -1052,11 +1105,13 @@ __device__ __forceinline__ void wide_tiles(const RowsArgs& a, int b, int kh, int
     const bool buffer = j == sq.nlist && sq.nt > 0;
     const int node = j - sq.nlist - (sq.nt > 0);
     __syncthreads();
-    if (buffer) {
-      wide_buffer<BITS>(a, u, L.tile[0]);
-    } else {
-      const bool bad = wide_nodes<BITS>(a, u, node, sq.tl, L.tile[0]);
-      if ((threadIdx.x & 63) == 0) L.bad[w] = bad;
+    if (w < 4) {
+      if (buffer) {
+        wide_buffer<BITS>(a, u, L.tile[0]);
+      } else {
+        const bool bad = wide_nodes<BITS>(a, u, node, sq.tl, L.tile[0]);
+        if ((threadIdx.x & 63) == 0) L.bad[w] = bad;
+      }
     }
     __syncthreads();
     if (!work) continue;
@@ -1082,20 +1137,16 @@ __device__ __forceinline__ void wide_tiles(const RowsArgs& a, int b, int kh, int
   }
 }
 
-__global__ __launch_bounds__(256, 2) void k_attn_wide(RowsArgs a) {
-  __shared__ __attribute__((aligned(16))) WideLds L;
+template <int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_attn_wide(RowsArgs a) {
+  __shared__ __attribute__((aligned(16))) WideLds<NW> L;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, g4 = lane >> 4;
-  const unsigned span = 8u * a.ntiles_row;  // (the row tiles of a chunk to one XCD)
-  const int rt = (int)(blockIdx.x % span >> 3);
-  int u = (int)(blockIdx.x / span * 8 + (blockIdx.x & 7));
-  const int s = u % a.nchunk;
-  u /= a.nchunk;
-  const int b = u / a.Hkv, kh = u - b * a.Hkv;
-  if (b >= a.B) return;
+  int b, kh, s, rt;
+  if (!rows_place(a, b, kh, s, rt)) return;
   const RowsSeq sq = rows_seq(a, b);
   const int rows = a.G * sq.tl;
-  if (kWideRows * rt >= rows || s >= max(sq.nparts, 1)) return;
-  const int base = kWideRows * rt + 32 * w;
+  if (kWideRows<NW> * rt >= rows || s >= max(sq.nparts, 1)) return;
+  const int base = kWideRows<NW> * rt + 32 * w;
   RowsQ<2> Q;
   RowsState<2> st;
 #pragma unroll
@@ -1114,9 +1165,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_wide(RowsArgs a) {
   const bool work = base < rows;
   if (j0 < j1) {
     if ((a.int2_mask >> kh) & 1ull)
-      wide_tiles<2>(a, b, kh, head_off, sq, j0, j1, work, Q, st, L);
+      wide_tiles<2, NW>(a, b, kh, head_off, sq, j0, j1, work, Q, st, L);
     else
-      wide_tiles<4>(a, b, kh, head_off, sq, j0, j1, work, Q, st, L);
+      wide_tiles<4, NW>(a, b, kh, head_off, sq, j0, j1, work, Q, st, L);
   }
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
@@ -1125,10 +1176,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_wide(RowsArgs a) {
     float* ws = a.ws + (Q.at[t] * a.nchunk + s) * kWsStride;
     if (sq.nparts > 1 && g4 == 0) *reinterpret_cast<float2*>(ws) = make_float2(st.m[t], l);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int c0 = 32 * g4 + 8 * r;
-      const float o[8] = {st.o[t][0][r], st.o[t][1][r], st.o[t][2][r], st.o[t][3][r],
-                          st.o[t][4][r], st.o[t][5][r], st.o[t][6][r], st.o[t][7][r]};
+    for (int e = 0; e < 4; ++e) {
+      const int c0 = 32 * e + 8 * g4;
+      const f4 x = st.o[t][2 * e], y = st.o[t][2 * e + 1];
+      const float o[8] = {x[0], y[0], x[1], y[1], x[2], y[2], x[3], y[3]};
       if (sq.nparts <= 1) {
         rows_store(a, Q.at[t], c0, st.m[t], l, o);
       } else {
@@ -1186,15 +1237,19 @@ __global__ __launch_bounds__(256) void k_rows_merge(RowsArgs a) {
 }
 
 // Query rows of a work-group: one or two tiles of 16 for every wave (the second shares
-// the codes' expansion), or 128 between them.
-inline int rows_tile(int G, int T) { return G * T <= 16 ? 16 : (G * T <= 64 ? 32 : kWideRows); }
+// the codes' expansion), or 32 a wave of four or eight.
+inline int rows_tile(int G, int T) {
+  const int rows = G * T;
+  return rows <= 16 ? 16 : rows <= 64 ? 32 : rows <= 512 ? kWideRows<4> : kWideRows<8>;
+}
 inline int rows_tiles_per_head(int G, int T) { return ceil_div(G * T, rows_tile(G, T)); }
 // Tiles of a chunk, at least: one a wave where the waves take tiles in turn.
-inline int rows_min_len(int G, int T) { return rows_tile(G, T) == kWideRows ? 8 : kRowsWaves; }
+inline int rows_min_len(int G, int T) { return rows_tile(G, T) > 32 ? 8 : kRowsWaves; }
 
-// Chunks of the grid: as many as give the GPU two work-groups per CU.
+// Chunks of the grid: as many as give the GPU two work-groups (of four waves) per CU.
 inline int rows_chunks(int B, int Hkv, int G, int T, int max_tiles) {
-  const long units = (long)B * Hkv * rows_tiles_per_head(G, T);
+  const int tile = rows_tile(G, T);
+  const long units = (long)B * Hkv * rows_tiles_per_head(G, T) * (tile > 128 ? 2 : 1);
   const long want = (512 + units - 1) / units;
   const long most = ceil_div(max_tiles, rows_min_len(G, T));
   return (int)(want < most ? (want > 1 ? want : 1) : (most > 1 ? most : 1));
@@ -1205,14 +1260,13 @@ inline long rows_groups(const RowsArgs& a) {
 }
 
 inline hipError_t launch_attn_rows(const RowsArgs& a, hipStream_t stream) {
-  const dim3 groups((unsigned)rows_groups(a)), threads(64 * kRowsWaves);
-  const int tile = rows_tile(a.G, a.T);
-  if (tile == 16)
-    hipLaunchKernelGGL((k_attn_rows<1>), groups, threads, 0, stream, a);
-  else if (tile == 32)
-    hipLaunchKernelGGL((k_attn_rows<2>), groups, threads, 0, stream, a);
-  else
-    hipLaunchKernelGGL(k_attn_wide, groups, threads, 0, stream, a);
+  const dim3 groups((unsigned)rows_groups(a));
+  switch (rows_tile(a.G, a.T)) {
+    case 16: hipLaunchKernelGGL((k_attn_rows<1>), groups, dim3(64 * kRowsWaves), 0, stream, a); break;
+    case 32: hipLaunchKernelGGL((k_attn_rows<2>), groups, dim3(64 * kRowsWaves), 0, stream, a); break;
+    case kWideRows<4>: hipLaunchKernelGGL((k_attn_wide<4>), groups, dim3(256), 0, stream, a); break;
+    default: hipLaunchKernelGGL((k_attn_wide<8>), groups, dim3(512), 0, stream, a); break;
+  }
   if (a.nchunk > 1) {
     const long rows = (long)a.B * a.Hq * a.T;
     hipLaunchKernelGGL(k_rows_merge, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a);

@@ -702,7 +702,7 @@ static int attn_rows_impl(turbo::RowsArgs& a, const turbo_kv_cache* cache,
   a.G = Hq / Hkv;
   a.ntiles_row = turbo::rows_tiles_per_head(a.G, T);
   a.nchunk = turbo::rows_chunks(B, Hkv, a.G, T, (int)tiles);
-  a.min_len = turbo::rows_min_len(a.G, T);
+  a.len = turbo::ceil_div((int)tiles, a.nchunk);
   if (turbo::rows_groups(a) > 0x7fffffffL) return TURBO_ERR_INVALID_ARG;
   const size_t need = rows_workspace(B, Hq, Hkv, T, tiles);
   if (need > 0 && (!workspace || workspace_bytes < need)) return TURBO_ERR_WORKSPACE_TOO_SMALL;
