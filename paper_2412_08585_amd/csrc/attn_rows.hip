@@ -31,6 +31,7 @@
 // are contiguous in every load, and a lane's outputs runs of 8 channels.
 #include "turbo_common.h"
 #include "stream_loads.h"
+#include <algorithm>
 
 namespace turbo {
 
@@ -101,8 +102,9 @@ __device__ __forceinline__ RowsSeq rows_seq(const RowsArgs& a, int b) {
 
 // The work of a work-group; false past the last.  They go to the eight XCDs in turn:
 // the row tiles of a chunk, which read the same codes, to one of them.  The first
-// chunks of all heads come first, the second ones after them: the chunks that short
-// sequences do not have lie together, not on some of the XCDs.
+// chunks of all heads come first, the second ones after them, so that the chunks that
+// short sequences do not have lie together, not on some of the XCDs; the heads, whose
+// bits and so whose work may differ, are rotated by the sequence.
 __device__ __forceinline__ bool rows_place(const RowsArgs& a, int& b, int& kh, int& s, int& rt) {
   const unsigned span = 8u * a.ntiles_row;
   rt = (int)(blockIdx.x % span >> 3);
@@ -110,7 +112,7 @@ __device__ __forceinline__ bool rows_place(const RowsArgs& a, int& b, int& kh, i
   s = u / (a.B * a.Hkv);
   const int bh = u - s * (a.B * a.Hkv);
   b = bh / a.Hkv;
-  kh = bh - b * a.Hkv;
+  kh = (bh - b * a.Hkv + b) % a.Hkv;
   return s < a.nchunk;
 }
 
@@ -1243,16 +1245,20 @@ inline int rows_tile(int G, int T) {
   return rows <= 16 ? 16 : rows <= 64 ? 32 : rows <= 512 ? kWideRows<4> : kWideRows<8>;
 }
 inline int rows_tiles_per_head(int G, int T) { return ceil_div(G * T, rows_tile(G, T)); }
-// Tiles of a chunk, at least: one a wave where the waves take tiles in turn.
-inline int rows_min_len(int G, int T) { return rows_tile(G, T) > 32 ? 8 : kRowsWaves; }
 
-// Chunks of the grid: as many as give the GPU two work-groups (of four waves) per CU.
+// Chunks of the grid: as many as give the GPU two work-groups of four waves per CU,
+// each with a tile for every wave (eight tiles where the waves share them), and more
+// where a long sequence's chunk would outlast the rest of a ragged batch.  A chunk's
+// state costs as much as about 8 tiles of 128 rows.  16 x 64/8 heads, ragged <= 257
+// tiles, 120 .. 504 rows: 1 chunk 555 us, 4 307, 8 (33 tiles) 289; 64 x 10 heads, 130
+// tiles of 20 rows: 1 chunk 193 us, 2 180, 3 189.
 inline int rows_chunks(int B, int Hkv, int G, int T, int max_tiles) {
   const int tile = rows_tile(G, T);
-  const long units = (long)B * Hkv * rows_tiles_per_head(G, T) * (tile > 128 ? 2 : 1);
-  const long want = (512 + units - 1) / units;
-  const long most = ceil_div(max_tiles, rows_min_len(G, T));
-  return (int)(want < most ? (want > 1 ? want : 1) : (most > 1 ? most : 1));
+  const bool wide = tile > 32;
+  const int units = (int)std::min<long>((long)B * Hkv * rows_tiles_per_head(G, T) * (tile > 128 ? 2 : 1), 512);
+  const int longest = !wide ? 72 : (units >= 256 ? 36 : max_tiles);
+  const int n = std::max(ceil_div(512, units), ceil_div(max_tiles, longest));
+  return std::max(1, std::min(n, ceil_div(max_tiles, wide ? 8 : kRowsWaves)));
 }
 
 inline long rows_groups(const RowsArgs& a) {
