@@ -700,7 +700,7 @@ static int attn_rows_impl(turbo::RowsArgs& a, const turbo_kv_cache* cache,
   a.Hkv = Hkv;
   a.T = T;
   a.G = Hq / Hkv;
-  a.ntiles_row = turbo::rows_tiles_per_head(a.G, T);
+  a.ntiles_row = turbo::rows_tiles_per_head(B, Hkv, a.G, T);
   a.nchunk = turbo::rows_chunks(B, Hkv, a.G, T, (int)tiles);
   a.len = turbo::ceil_div((int)tiles, a.nchunk);
   if (turbo::rows_groups(a) > 0x7fffffffL) return TURBO_ERR_INVALID_ARG;
