@@ -74,6 +74,8 @@ struct RowsArgs {
 };
 
 constexpr int kRowsWaves = 4;   // waves of a work-group, a tile each in turn
+constexpr int kRowsLongest = 72;  // tiles of a chunk, at most, where waves take them in turn
+static_assert(kRowsLongest / kRowsWaves < 64, "a chunk's tables are held by a wave");
 constexpr float kPShift = 7.0f;
 
 // The tiles of sequence b: cached groups (or choices), the buffer, the nodes.
@@ -301,9 +303,8 @@ __device__ __forceinline__ void value_scale(float sv, float up, float& ex, float
 }
 
 // ---- a cached group ------------------------------------------------------------
-// Table entries and scales of the wave's next 64 tiles, lane i holding the i-th: one
-// round of loads for 64 steps, and no step waits for a table entry before its codes
-// can leave.
+// Table entries and scales of 64 tiles, lane i holding the i-th: one round of loads for
+// 64 steps, and no step waits for a table entry before its codes can leave.
 struct RowsTab {
   int pg[4];     // pages, 0 where there is nothing to attend
   int slot;      // -1 where there is nothing to attend
@@ -698,7 +699,7 @@ __device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int
   const int je = min(j1, sq.nlist);
   if (j < je) {
     load_q<NT, BITS == 4 ? kOrd4 : kOrd2>(a, Q);
-    const int cnt = ceil_div(je - j, kRowsWaves);
+    const int cnt = ceil_div(je - j, kRowsWaves);  // (kRowsLongest / kRowsWaves at most)
     RowsTab T;
     load_tab<kRowsWaves>(a, b, kh, sq, j, je, T);
     RowsGroup<BITS> x;
@@ -706,14 +707,12 @@ __device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int
     load_group_v<BITS>(a, kh, head_off, T, 0, x);
     // each half's next codes are requested as soon as its registers are free
     for (int i = 0; i < cnt; ++i) {
-      const int at = i & 63;
-      const bool live = __builtin_amdgcn_readlane(T.slot, at) >= 0;
-      const float sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sk), at));
-      const float sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sv), at));
-      if (at == 63) load_tab<kRowsWaves>(a, b, kh, sq, j + kRowsWaves * (i + 1), je, T);
+      const bool live = __builtin_amdgcn_readlane(T.slot, i) >= 0;
+      const float sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sk), i));
+      const float sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sv), i));
       f4 S[NT][4];
       group_scores<BITS, NT>(x, Q, S, szk);
-      load_group_k<BITS>(a, kh, head_off, T, (i + 1) & 63, x);
+      load_group_k<BITS>(a, kh, head_off, T, i + 1, x);
       if (live) {
         constexpr float up = 1 << kDown<BITS>;
         float ex, inv;
@@ -724,7 +723,7 @@ __device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int
           rows_softmax<NT, BITS == 4, false>(st, t, S[t], sk * (a.sm_log2e * up), ex, inv, 0, P[t]);
         group_values<BITS, NT>(x, P, st, szv);
       }
-      load_group_v<BITS>(a, kh, head_off, T, (i + 1) & 63, x);
+      load_group_v<BITS>(a, kh, head_off, T, i + 1, x);
     }
     j += kRowsWaves * cnt;
   }
@@ -1262,7 +1261,7 @@ inline int rows_chunks(int B, int Hkv, int G, int T, int max_tiles) {
   const int tile = rows_tile(B, Hkv, G, T);
   const bool wide = tile > 32;
   const int units = (int)std::min<long>((long)B * Hkv * rows_tiles_per_head(B, Hkv, G, T) * (tile > 128 ? 2 : 1), 512);
-  const int longest = !wide ? 72 : (units >= 256 ? 36 : max_tiles);
+  const int longest = !wide ? kRowsLongest : (units >= 256 ? 36 : max_tiles);
   const int n = std::max(ceil_div(!wide && units <= 32 ? 256 : 512, units), ceil_div(max_tiles, longest));
   return std::max(1, std::min(n, ceil_div(max_tiles, wide ? 8 : kRowsWaves)));
 }

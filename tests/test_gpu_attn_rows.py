@@ -89,6 +89,8 @@ TREES = [
     (1, 4, 1, [2], [64 * 140 + 9], 30, [30], "tree", True),     # past 64 table entries
     (1, 2, 1, [4], [64 * 66], 64, [64], "any", False),
     (2, 16, 1, [4], [64 * 4 + 2, 64 * 17], 8, [8, 5], "tree", True),
+    (2, 12, 2, [4, 2], [64 * 9 + 5, 64 * 70 + 1], 100, [100, 37], "any", True),  # 600 rows
+    (1, 16, 1, [2], [64 * 20 + 63], 64, [64], "tree", False),
     (9, 8, 8, [4, 2] * 4, [64 * i + 7 * i for i in range(9)], 4, [4, 3, 2, 1, 0, 4, 4, 4, 4], "tree", True),
 ]
 
@@ -306,6 +308,37 @@ def test_selected_every_group_is_near_the_decode(ta, dev):
     d, dl = ta.turbo_attn_decode(q, f.cache, f.sl, f.btd, f.gtd, tail=f.tail, return_lse=True)
     assert ((o - d).float().norm() / d.float().norm()).item() < 0.1
     assert (lse - dl).abs().max().item() < 0.1
+
+
+@pytest.mark.parametrize("B,T", [(32, 66), (33, 20), (8, 260 // 2), (4, 3)])
+def test_long_sequences_in_a_batch(ta, dev, B, T):
+    """Chunks of more tiles than one round of table entries: B sequences that are the
+    same one of 18000 tokens, four of its rows against 64 bits, all alike."""
+    Hkv, Hq, bits = 4, 8 if T == 130 else 4, [4, 2, 2, 4]
+    f = ref.Filled(ta, dev, [18000], bits, seed=97)
+    q, kt, vt = ref.rand((1, Hq, T, D), 1), ref.rand((1, Hkv, T, D), 2), ref.rand((1, Hkv, T, D), 3)
+    see = _trees("tree", 1, T, [T], 3)
+    tail = ta.KVTail(B, Hkv, dev)
+    for x, y in ((tail.k, f.tail.k), (tail.v, f.tail.v), (tail.scale, f.tail.scale)):
+        x.copy_(y.expand(x.shape))
+
+    def all_of(x):
+        return x.to(dev).expand(B, *x.shape[1:]).contiguous()
+
+    o, lse = ta.turbo_attn_tree(all_of(q), all_of(kt), all_of(vt), all_of(_words(see, dev)),
+                                torch.full((B,), T, dtype=torch.int32, device=dev), f.cache,
+                                all_of(f.sl[None])[:, 0].contiguous(), all_of(f.btd), all_of(f.gtd),
+                                tail=tail, return_lse=True)
+    assert torch.equal(o, o[:1].expand_as(o)) and torch.equal(lse, lse[:1].expand_as(lse))
+    f.host()
+    for h in range(Hkv):
+        k, v = f.kv(0, h, range(f.groups(0)))
+        k, v = np.concatenate([k, kt[0, h].double().numpy()]), np.concatenate([v, vt[0, h].double().numpy()])
+        r, i = h * (Hq // Hkv), [0, T // 2, T - 1]
+        vis = np.concatenate([np.ones((T, len(k) - T), bool), see[0]], 1)[i]
+        w, wl, to, tol = ref.attend(q[0, r, i].double().numpy(), k, v, vis)
+        _check(o[0, r, i].double().cpu().numpy(), w, to, f"o {h}")
+        _check(lse[0, r, i].double().cpu().numpy(), wl, tol, f"lse {h}")
 
 
 def test_long_cache_past_32_bit_offsets(ta, dev):
