@@ -564,6 +564,7 @@ size_t turbo_select_workspace_bytes(int B, int Hq, int max_groups_per_seq);
  *                 sequence's full groups) is skipped, as is a group whose table
  *                 entries are out of range; a group named twice counts twice.
  * num_select      >= 1.
+ * sm_scale        positive, at most 1e30.
  * workspace       device scratch of turbo_selected_workspace_bytes() bytes
  *                 (may be NULL when that is 0; no initialization needed); calls
  *                 that share it must not overlap.
@@ -621,6 +622,7 @@ int turbo_tree_mask(const int32_t* parents, const int32_t* tree_lens, int B, int
  * cache, tail, seq_lens, block_table, group_table, max_groups_per_seq
  *            as for turbo_attn_decode.
  * T          1 .. TURBO_MAX_TREE.
+ * sm_scale   positive, at most 1e30.
  * workspace  device scratch of turbo_tree_workspace_bytes() bytes (may be NULL
  *            when that is 0; no initialization needed); calls that share it
  *            must not overlap.

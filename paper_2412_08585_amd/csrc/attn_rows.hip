@@ -294,10 +294,12 @@ __device__ __forceinline__ void rows_softmax(RowsState<NT>& st, int t, f4 (&S)[4
       P[ks][jj] = PAIR4 ? h2_of(S[2 * ks][jj], S[2 * ks + 1][jj]) : h2_of(S[ks][jj], S[ks + 2][jj]);
 }
 
-// log2 and inverse of the scale of a tile's V (times 2^down); a scale of zero has
-// only zeros behind it and counts as one.
+// log2 and inverse of the scale of a tile's V, brought to its operands.  Below 2^-60
+// (zero, or a scale whose values all round to zero in fp16) it counts as 2^-60, which
+// both functions and the sums stand.
 __device__ __forceinline__ void value_scale(float sv, float up, float& ex, float& inv) {
-  const float s = sv == 0.0f ? 1.0f : sv * up;
+  float s = sv * up;
+  s = s < 0x1p-60f ? 0x1p-60f : s;  // (NaN stays)
   ex = __builtin_amdgcn_logf(s);
   inv = __builtin_amdgcn_rcpf(s);
 }

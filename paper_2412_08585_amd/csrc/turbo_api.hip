@@ -730,7 +730,7 @@ static int attn_rows_impl(turbo::RowsArgs& a, const turbo_kv_cache* cache,
 static bool rows_heads_ok(const turbo_kv_cache* cache, int B, int Hq, int max_groups_per_seq,
                           float sm_scale) {
   if (!cache || B < 0 || Hq < 1 || max_groups_per_seq < 1 || !(sm_scale > 0.0f) ||
-      sm_scale > 2.0e38f)
+      sm_scale > 1.0e30f)
     return false;
   const int Hkv = cache->num_kv_heads;
   return Hkv >= 1 && Hkv <= TURBO_MAX_KV_HEADS && Hq % Hkv == 0 && Hq / Hkv <= TURBO_MAX_GQA;

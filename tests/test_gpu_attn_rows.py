@@ -223,6 +223,36 @@ def test_tree_skips_groups_outside_the_tables_ranges(ta, dev):
     _check_tree(f, q, kt, vt, see, [T] * B, o, lse)
 
 
+@pytest.mark.parametrize("Hq,T", [(2, 3), (4, 24), (4, 90)])
+def test_scales_of_zero_and_far_apart(ta, dev, Hq, T):
+    """Groups and buffers whose scales are zero, subnormal or far from the others'."""
+    B, Hkv = 2, 2
+    f = ref.Filled(ta, dev, [64 * 14 + 20, 64 * 3 + 5], [4, 2], seed=65)
+    sc = f.cache.group_scale
+    for i, (sk, sv) in enumerate([(None, 0.0), (0.0, None), (None, 1e-42), (1e-42, None), (None, 1e-30),
+                                  (None, 50.0), (0.0, 0.0), (None, 1e-4)]):
+        slot = f.gtd[0, i].long()
+        if sk is not None:
+            sc[slot, :, 0] = sk
+        if sv is not None:
+            sc[slot, :, 1] = sv
+    sc[f.gtd[1].long()[:3], :, 1] = torch.tensor([0.0, 1e-42, 0.0], device=dev)[:, None]
+    f.tail.scale[0, 0], f.tail.scale[1, 0], f.tail.scale[1, 1, 1] = 0.0, 1e-42, 0.0
+    q, kt, vt = ref.rand((B, Hq, T, D), 1), ref.rand((B, Hkv, T, D), 2), ref.rand((B, Hkv, T, D), 3)
+    see = _trees("any", B, T, [T] * B, 3)
+    o, lse = ta.turbo_attn_tree(q.to(dev), kt.to(dev), vt.to(dev), _words(see, dev),
+                                torch.tensor([T, T], dtype=torch.int32, device=dev), f.cache, f.sl,
+                                f.btd, f.gtd, tail=f.tail, return_lse=True)
+    _check_tree(f, q, kt, vt, see, [T] * B, o, lse)
+    # no number in the scale of one group: none in the rows that attend it
+    sc[f.gtd[0, 9].long(), 1, 1] = float("nan")
+    o2, lse2 = ta.turbo_attn_tree(q.to(dev), kt.to(dev), vt.to(dev), _words(see, dev),
+                                  torch.tensor([T, T], dtype=torch.int32, device=dev), f.cache, f.sl,
+                                  f.btd, f.gtd, tail=f.tail, return_lse=True)
+    G = Hq // Hkv
+    assert torch.isnan(o2[0, G:]).all() and torch.equal(o2[0, :G], o[0, :G]) and torch.equal(o2[1], o[1])
+
+
 def test_operands_at_any_fp16_boundary(ta, dev):
     B, Hq, Hkv, T = 1, 4, 2, 20
     f = ref.Filled(ta, dev, [64 * 4 + 10], [4, 2], seed=71)
