@@ -67,15 +67,13 @@ struct RowsArgs {
   const float* tscale;
   int ntiles_row;            // row tiles in the grid
   int nchunk;                // chunks in the grid
-  int len;                   // tiles of a chunk
+  int min_len;               // tiles of a chunk, at least
   float* ws;                 // [B][Hq][T][nchunk][132]: m, l, -, -, O[128]
   unsigned short* o;         // fp16 [B][Hq][T][128]
   float* lse;                // [B][Hq][T] or null
 };
 
 constexpr int kRowsWaves = 4;   // waves of a work-group, a tile each in turn
-constexpr int kRowsLongest = 72;  // tiles of a chunk, at most, where waves take them in turn
-static_assert(kRowsLongest / kRowsWaves < 64, "a chunk's tables are held by a wave");
 constexpr float kPShift = 7.0f;
 
 // The tiles of sequence b: cached groups (or choices), the buffer, the nodes.
@@ -97,7 +95,7 @@ __device__ __forceinline__ RowsSeq rows_seq(const RowsArgs& a, int b) {
   s.tl = a.tree_lens ? min(max(a.tree_lens[b], 0), a.T) : a.T;
   s.nlist = a.sel ? a.nsel : s.ng;
   s.ntile = s.nlist + (s.nt > 0) + (a.kt ? (s.tl + 63) / 64 : 0);
-  s.len = a.len;
+  s.len = max(a.min_len, ceil_div(s.ntile, a.nchunk));
   s.nparts = ceil_div(s.ntile, s.len);
   return s;
 }
@@ -701,7 +699,7 @@ __device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int
   const int je = min(j1, sq.nlist);
   if (j < je) {
     load_q<NT, BITS == 4 ? kOrd4 : kOrd2>(a, Q);
-    const int cnt = ceil_div(je - j, kRowsWaves);  // (kRowsLongest / kRowsWaves at most)
+    const int cnt = ceil_div(je - j, kRowsWaves);
     RowsTab T;
     load_tab<kRowsWaves>(a, b, kh, sq, j, je, T);
     RowsGroup<BITS> x;
@@ -709,12 +707,14 @@ __device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int
     load_group_v<BITS>(a, kh, head_off, T, 0, x);
     // each half's next codes are requested as soon as its registers are free
     for (int i = 0; i < cnt; ++i) {
-      const bool live = __builtin_amdgcn_readlane(T.slot, i) >= 0;
-      const float sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sk), i));
-      const float sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sv), i));
+      const int at = i & 63, next = (i + 1) & 63;
+      const bool live = __builtin_amdgcn_readlane(T.slot, at) >= 0;
+      const float sk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sk), at));
+      const float sv = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T.sv), at));
+      if (next == 0) load_tab<kRowsWaves>(a, b, kh, sq, j + kRowsWaves * (i + 1), je, T);
       f4 S[NT][4];
       group_scores<BITS, NT>(x, Q, S, szk);
-      load_group_k<BITS>(a, kh, head_off, T, i + 1, x);
+      load_group_k<BITS>(a, kh, head_off, T, next, x);
       if (live) {
         constexpr float up = 1 << kDown<BITS>;
         float ex, inv;
@@ -725,7 +725,7 @@ __device__ __forceinline__ void rows_tiles(const RowsArgs& a, int b, int kh, int
           rows_softmax<NT, BITS == 4, false>(st, t, S[t], sk * (a.sm_log2e * up), ex, inv, 0, P[t]);
         group_values<BITS, NT>(x, P, st, szv);
       }
-      load_group_v<BITS>(a, kh, head_off, T, i + 1, x);
+      load_group_v<BITS>(a, kh, head_off, T, next, x);
     }
     j += kRowsWaves * cnt;
   }
@@ -1252,20 +1252,29 @@ inline int rows_tiles_per_head(int B, int Hkv, int G, int T) {
   return ceil_div(G * T, rows_tile(B, Hkv, G, T));
 }
 
-// Chunks of the grid: as many as give the GPU two work-groups of four waves per CU (one
-// where few heads have to fill it, so that fewer states are merged: 13.9 us against
-// 16.0 in the case above), each with a tile for every wave (eight tiles where the waves share them), and more
-// where a long sequence's chunk would outlast the rest of a ragged batch.  A chunk's
-// state costs as much as about 8 tiles of 128 rows.  16 x 64/8 heads, ragged <= 257
-// tiles, 120 .. 504 rows: 1 chunk 555 us, 4 307, 8 (33 tiles) 289; 64 x 10 heads, 130
-// tiles of 20 rows: 1 chunk 193 us, 2 180, 3 189.
-inline int rows_chunks(int B, int Hkv, int G, int T, int max_tiles) {
+// Chunks of a sequence, at most, and their tiles, at least.  As many as give the GPU two
+// work-groups of four waves per CU (one where few heads have to fill it, so that fewer
+// states are merged: 13.9 us against 16.0 in the case above), with a tile for every
+// wave (eight where the waves share them).  Where the heads fill the GPU by themselves,
+// up to 16 chunks of 32 tiles or more, so that a long sequence does not outlast the rest
+// of a ragged batch; a chunk's state costs as much as about 8 tiles of 128 rows.  16 x
+// 64/8 heads, ragged <= 257 tiles, 120 .. 504 rows: 1 chunk 555 us, 4 307, 8 (33 tiles)
+// 289; 64 x 10 heads, 130 tiles of 20 rows: 1 chunk 193 us, 2 180, 3 189.  The tables'
+// width bounds the chunks, the sequence's own length divides them.
+struct RowsSplit {
+  int chunks, min_len;
+};
+inline RowsSplit rows_split(int B, int Hkv, int G, int T, int max_tiles) {
   const int tile = rows_tile(B, Hkv, G, T);
   const bool wide = tile > 32;
   const int units = (int)std::min<long>((long)B * Hkv * rows_tiles_per_head(B, Hkv, G, T) * (tile > 128 ? 2 : 1), 512);
-  const int longest = !wide ? kRowsLongest : (units >= 256 ? 36 : max_tiles);
-  const int n = std::max(ceil_div(!wide && units <= 32 ? 256 : 512, units), ceil_div(max_tiles, longest));
-  return std::max(1, std::min(n, ceil_div(max_tiles, wide ? 8 : kRowsWaves)));
+  RowsSplit r = {ceil_div(!wide && units <= 32 ? 256 : 512, units), wide ? 8 : kRowsWaves};
+  if (units >= 256) {
+    r.chunks = std::max(r.chunks, std::min(16, ceil_div(max_tiles, wide ? 36 : 72)));
+    r.min_len = 32;
+  }
+  r.chunks = std::max(1, std::min(r.chunks, ceil_div(max_tiles, r.min_len)));
+  return r;
 }
 
 inline long rows_groups(const RowsArgs& a) {

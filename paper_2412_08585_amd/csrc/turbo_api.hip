@@ -664,7 +664,7 @@ int turbo_select_groups(const void* q, const turbo_kv_cache* cache, const int32_
 // Tiles of 64 tokens the longest sequence can have, and the workspace for them.
 static size_t rows_workspace(int B, int Hq, int Hkv, int T, long tiles) {
   if (tiles > 0x7fffffffL) return 0;
-  const int n = turbo::rows_chunks(B, Hkv, Hq / Hkv, T, (int)tiles);
+  const int n = turbo::rows_split(B, Hkv, Hq / Hkv, T, (int)tiles).chunks;
   return n > 1 ? (size_t)B * Hq * T * n * turbo::kWsStride * sizeof(float) : 0;
 }
 
@@ -701,8 +701,9 @@ static int attn_rows_impl(turbo::RowsArgs& a, const turbo_kv_cache* cache,
   a.T = T;
   a.G = Hq / Hkv;
   a.ntiles_row = turbo::rows_tiles_per_head(B, Hkv, a.G, T);
-  a.nchunk = turbo::rows_chunks(B, Hkv, a.G, T, (int)tiles);
-  a.len = turbo::ceil_div((int)tiles, a.nchunk);
+  const turbo::RowsSplit split = turbo::rows_split(B, Hkv, a.G, T, (int)tiles);
+  a.nchunk = split.chunks;
+  a.min_len = split.min_len;
   if (turbo::rows_groups(a) > 0x7fffffffL) return TURBO_ERR_INVALID_ARG;
   const size_t need = rows_workspace(B, Hq, Hkv, T, tiles);
   if (need > 0 && (!workspace || workspace_bytes < need)) return TURBO_ERR_WORKSPACE_TOO_SMALL;

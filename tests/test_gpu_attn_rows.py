@@ -371,6 +371,45 @@ def test_long_sequences_in_a_batch(ta, dev, B, T):
         _check(lse[0, r, i].double().cpu().numpy(), wl, tol, f"lse {h}")
 
 
+@pytest.mark.parametrize("B,Hkv,T,ng", [(64, 4, 1, 5200), (1, 2, 40, 700), (8, 4, 70, 5000)])
+def test_very_long_tables(ta, dev, B, Hkv, T, ng):
+    """Sequences of up to 333000 tokens (three groups of keys and values over and over),
+    beside short ones in tables as wide: every round of table entries, every chunk."""
+    bits = [4, 2] * (Hkv // 2)
+    f = ref.Filled(ta, dev, [64 * 3], bits, seed=99, tail=False)
+    kind = np.random.default_rng(ng).integers(0, 3, ng)
+    count = np.bincount(kind, minlength=3)
+    gt = np.repeat(f.gt[0][kind][None], B, 0).astype(np.int32)
+    bt = np.repeat(f.bt[0].reshape(-1, 4)[kind].reshape(1, -1), B, 0).astype(np.int32)
+    lens = [64 * ng if b % 3 == 0 else 64 * (b % 7) for b in range(B)]
+    q, kt, vt = (ref.rand((1, Hkv, T, D), i).expand(B, -1, -1, -1).contiguous() for i in (1, 2, 3))
+    i32 = dict(dtype=torch.int32, device=dev)
+    o, lse = ta.turbo_attn_tree(q.to(dev), kt.to(dev), vt.to(dev), None, torch.full((B,), T, **i32),
+                                f.cache, torch.tensor(lens, **i32), torch.from_numpy(bt).to(dev),
+                                torch.from_numpy(gt).to(dev), return_lse=True)
+    f.host()
+    for b in sorted({0, 1 % B, 2 % B, B - 1}):
+        n = lens[b] // 64
+        c = np.bincount(kind[:n], minlength=3)
+        for h in range(Hkv):
+            k, v = f.kv(0, h, range(3))
+            for i in sorted({0, T // 2, T - 1}):
+                # a token seen c times weighs c times: its score plus ln c
+                kk = np.concatenate([k, kt[b, h, :i + 1].double().numpy()])
+                vv = np.concatenate([v, vt[b, h, :i + 1].double().numpy()])
+                w = np.concatenate([np.repeat(c, 64), np.ones(i + 1)])
+                x = ref.SM * (kk @ q[b, h, i].double().numpy())
+                p = np.exp(x - x.max()) * w
+                want, l = p @ vv / p.sum(), x.max() + np.log(p.sum())
+                _, _, to, tol = ref.attend(q[b, h, i:i + 1].double().numpy(), kk, vv)
+                # (n tokens instead of a few hundred in the row's sums)
+                more = (w.sum() / 16) * 2.0 ** -24
+                a = p @ np.abs(vv) / p.sum()
+                to = ref.F16 * np.abs(want) + 2.0 ** -25 + a * (ref.F16 + more + 2.0 ** -19)
+                _check(o[b, h, i].double().cpu().numpy(), want, to, f"o {b} {h} {i}")
+                assert abs(lse[b, h, i].item() - l) <= tol[0] + more + 2.0 ** -22 * abs(l)
+
+
 def test_long_cache_past_32_bit_offsets(ta, dev):
     """Pages beyond 4 GiB of the pool."""
     bits = [4] * 64
