@@ -7,6 +7,10 @@
 // is the largest sum any key of the group could reach: an integer, two dot products
 // over the 256 metadata bytes of the group's K, 3 % (4 bits) of what attending the
 // group reads.  fl(fl(I * s_Q) * s_K) bounds the score up to the common factor.
+//
+// A few hundred bytes to a megabyte in all: bound by a chain of latencies, not by bytes
+// or sums.  511 groups of 8 heads, 64 chosen, 9.7 us; 32 x 8 heads of up to 255 groups,
+// eight rows, 11.5 us; with bounds and choice in two launches 14.4 and 16.5.
 #include "turbo_common.h"
 
 namespace turbo {

@@ -36,6 +36,8 @@ SELECTS = [
     (32, [2, 4], [64 * 300 + 1, 64 * 257, 64 * 256], 100, 1, 2),
     (10, [4, 2], [64 * 20], 30, 0, 0),           # more than there are
     (6, [2, 4, 4], [64 * 40, 64], 1, 1, 0),      # kept groups alone
+    (4, [4, 2], [64 * 700 + 3, 64 * 513], 128, 1, 1),
+    (2, [4], [64 * 1030], 40, 0, 3),             # bounds and choice in launches of their own
 ]
 
 
@@ -71,6 +73,20 @@ def test_select_many_equal_scores(ta, dev):
         got = ta.turbo_select_groups(q.to(dev), f.cache, sl, torch.from_numpy(f.bt).to(dev),
                                      torch.from_numpy(f.gt).to(dev), num, 1, 0)
         assert (got.cpu().numpy() == ref.select(f, q.numpy(), num, 1, 0)).all(), num
+
+
+def test_select_many_heads_of_long_tables(ta, dev):
+    """256 KV heads of 1100 groups (three kinds, over and over): one launch."""
+    f = ref.Filled(ta, dev, [64 * 3], [4, 2] * 32, seed=6).host()
+    mg, B = 1100, 4
+    kind = np.random.default_rng(2).integers(0, 3, (B, mg))
+    f.mg, f.lens = mg, [64 * mg, 64 * 900 + 5, 64 * 1025, 70]
+    f.gt = f.gt[0][kind].astype(np.int32)
+    f.bt = f.bt[0].reshape(-1, 4)[kind].reshape(B, -1).astype(np.int32)
+    q = ref.rand((B, 64, D), 3)
+    got = ta.turbo_select_groups(q.to(dev), f.cache, torch.tensor(f.lens, dtype=torch.int32, device=dev),
+                                 torch.from_numpy(f.bt).to(dev), torch.from_numpy(f.gt).to(dev), 77, 1, 2)
+    assert (got.cpu().numpy() == ref.select(f, q.numpy(), 77, 1, 2)).all()
 
 
 def test_select_scores_that_are_no_numbers(ta, dev):
