@@ -1199,24 +1199,26 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attn_wide(RowsArgs a) {
   }
 }
 
-// Rows of several chunks: a wave merges a row's states, a quarter of them in each 16
-// lanes (four at a time, their loads together), then the quarters.
+// Rows of several chunks.  Q groups of 16 lanes merge a row's states, each every Q-th
+// (four at a time, their loads together), then the groups: a wave a row where few rows
+// have many states, four rows a wave otherwise.
+template <int Q>
 __global__ __launch_bounds__(256) void k_rows_merge(RowsArgs a) {
-  const long at = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (at >= (long)a.B * a.Hq * a.T) return;
   const int lane = threadIdx.x & 63, c0 = 8 * (lane & 15);
+  const long at = ((long)blockIdx.x * 16 + (threadIdx.x >> 4)) / Q;
+  if (at >= (long)a.B * a.Hq * a.T) return;
   const long bh = at / a.T;
   const int b = (int)(bh / a.Hq);
   const RowsSeq sq = rows_seq(a, b);
   if (at - bh * a.T >= sq.tl || sq.nparts <= 1) return;
   const float* ws = a.ws + at * a.nchunk * kWsStride;
   float m = -INFINITY, l = 0.0f, o[8] = {};
-  for (int i0 = lane >> 4; i0 < sq.nparts; i0 += 16) {
+  for (int i0 = (lane >> 4) % Q; i0 < sq.nparts; i0 += 4 * Q) {
     float pm[4], pl[4];
     float4 x[4], y[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int i = i0 + 4 * k;
+      const int i = i0 + Q * k;
       pm[k] = -INFINITY;
       pl[k] = 0.0f;
       x[k] = y[k] = make_float4(0, 0, 0, 0);
@@ -1235,14 +1237,14 @@ __global__ __launch_bounds__(256) void k_rows_merge(RowsArgs a) {
     }
   }
 #pragma unroll
-  for (int d = 16; d <= 32; d += d) {
+  for (int d = 16; d < 16 * Q; d += d) {
     float v[8];
     const float pm = __shfl_xor(m, d), pl = __shfl_xor(l, d);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = __shfl_xor(o[e], d);
     rows_join(m, l, o, pm, pl, v);
   }
-  if (lane < 16) rows_store(a, at, c0, m, l, o);
+  if (Q == 1 || lane < 16) rows_store(a, at, c0, m, l, o);
 }
 
 // Query rows of a work-group: one or two tiles of 16 for every wave (the second shares
@@ -1297,7 +1299,10 @@ inline hipError_t launch_attn_rows(const RowsArgs& a, hipStream_t stream) {
   }
   if (a.nchunk > 1) {
     const long rows = (long)a.B * a.Hq * a.T;
-    hipLaunchKernelGGL(k_rows_merge, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a);
+    if (rows <= 4096)
+      hipLaunchKernelGGL((k_rows_merge<4>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, a);
+    else
+      hipLaunchKernelGGL((k_rows_merge<1>), dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, stream, a);
   }
   return hipGetLastError();
 }
