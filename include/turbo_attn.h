@@ -571,7 +571,8 @@ size_t turbo_select_workspace_bytes(int B, int Hq, int max_groups_per_seq);
  * o               fp16 [B][Hq][128];  lse fp32 [B][Hq] or NULL.  A row that
  *                 attends no token yields o = 0 and lse = -inf.
  * The same call on the same inputs gives the same bits; the order of the sums
- * (not the result beyond rounding) depends on the shapes of the call.
+ * (not the result beyond rounding) depends on the shapes of the call.  Errors as
+ * turbo_attn_decode.
  */
 int turbo_attn_selected(const void* q, const turbo_kv_cache* cache, const turbo_kv_tail* tail,
                         const int32_t* seq_lens, const int32_t* block_table,
@@ -630,7 +631,8 @@ int turbo_tree_mask(const int32_t* parents, const int32_t* tree_lens, int B, int
  *            attends no token yields o = 0 and lse = -inf.  Rows of nodes past
  *            a tree's last are left as they were.
  * A key or value of a node that a row does not attend, and anything past the
- * tree's last node, has no effect on it, be it infinite or NaN.
+ * tree's last node, has no effect on it, be it infinite or NaN.  Errors as
+ * turbo_attn_decode, and INVALID_ARG for T outside its range.
  */
 int turbo_attn_tree(const void* q, const void* k_tree, const void* v_tree,
                     const uint64_t* tree_mask, const int32_t* tree_lens,

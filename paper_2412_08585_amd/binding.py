@@ -577,9 +577,9 @@ def _launch(index: int, what: str, *args):
     """The library's `what` with args and the device's current stream, on that device."""
     if index < 0:
         raise ValueError("Expected tensors on a cuda device")
-    fn = getattr(lib(), what)
+    fn = getattr(_lib or lib(), what)
     stream = torch._C._cuda_getCurrentRawStream(index)
-    if index == torch.cuda.current_device():
+    if index == torch._C._cuda_getDevice():
         status = fn(*args, stream)
     else:
         with torch.cuda.device(index):
